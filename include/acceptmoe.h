@@ -80,6 +80,8 @@ extern "C" {
 #define ACCEPTMOE_MAX_TOPK 32
 #define ACCEPTMOE_MAX_TREES 256
 #define ACCEPTMOE_MAX_TREE_NODES 1024
+#define ACCEPTMOE_MAX_VOCAB (1 << 20)
+#define ACCEPTMOE_MAX_SAMPLE_ROWS (1 << 20)
 /* static scratch of acceptmoe_select_noalloc per device: 8 MiB (e.g. up to
  * 7,000 nodes at E = 128, k = 8; acceptmoe_select_workspace_size gives the need) */
 #define ACCEPTMOE_SELECT_NOALLOC_MAX_WORKSPACE ((size_t)8 << 20)
@@ -294,6 +296,89 @@ int32_t acceptmoe_moe_forward(const void* hidden, int32_t dtype, const void* w_g
  */
 int32_t acceptmoe_residual_add(const void* hidden, int32_t dtype, const float* y, int32_t T,
                                int32_t H, void* out, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Around the layer: what stands between two layers and behind the last
+ * ---------------------------------------------------------------------------
+ * acceptmoe_residual_norm -- acceptmoe_residual_add with the root-mean-square
+ * norm behind it, which makes the next layer's input in one pass:
+ *   s = hidden + y (fp32), hidden_out = s rounded to `dtype`,
+ *   n = s / sqrt(mean_h s^2 + eps) * weight   (fp32, from the unrounded s).
+ * group == 0: norm_out [T, H] of `dtype`, n rounded once (to nearest even).
+ * group != 0: norm_out [T, H] holds n in 8 bits (e4m3: 4 exponent and 3
+ * mantissa bits, largest value 448) and scale_out one fp32 scale per `group`
+ * columns ([T, H / group]) or per row (group == -1: [T]):
+ *   scale = max |n| / 448,  code = e4m3(n / scale)   (0 where scale is 0),
+ * so scale * code stands for n.
+ *   hidden      [T, H] device, `dtype`
+ *   y           [T, H] device fp32, or NULL: no addend, s = hidden, and
+ *               hidden_out is neither needed nor written
+ *   weight      [H] device, `dtype`
+ *   hidden_out  [T, H] device, `dtype`; may equal hidden
+ *   norm_out    must overlap no input; scale_out is unused when group == 0
+ *   H % 4 == 0, H <= 65536, eps finite and >= 0; group 0, -1, 32, 64, 128 or 256
+ *   and a divisor of H.  All pointers 16-byte aligned (scale_out: 4).
+ * The sum of squares is held in fp32, in a fixed order (deterministic).
+ */
+int32_t acceptmoe_residual_norm(const void* hidden, int32_t dtype, const float* y, const void* weight, int32_t T,
+                                int32_t H, float eps, int32_t group, void* hidden_out, void* norm_out,
+                                float* scale_out, void* stream);
+
+/*
+ * acceptmoe_sample -- a token for every row of logits from a given random number.
+ * A row's tokens stand in the order (logit descending, index ascending), with
+ * w_j = exp((z_j - max z) / temperature) and C_j the sum of the first j weights.
+ * The filters keep a prefix of that order, one after the other:
+ *   top_k   the first top_k tokens (<= 0: all)
+ *   top_p   the shortest prefix with C_j >= top_p * C of what top_k left, at
+ *           least one token (>= 1: all)
+ *   min_p   of these the tokens with w_j >= min_p (<= 0: all; above 1 counts as 1)
+ * token[r] is the first kept j with C_j > u C_kept, prob[r] = w_j / C_kept its
+ * probability.  temperature <= 0 (or NaN): the largest logit's token (the lowest
+ * index of equal ones), prob 1.
+ * Tokens whose logit is -inf or NaN are never chosen; a row without any other gives
+ * token -1 and prob 0.  Where logits are +inf, those tokens share the weight.
+ *   logits       [R, V] device, `dtype` (F32 or BF16), row r at element
+ *                r * row_stride (>= V), aligned to its element
+ *   uniform      [R] device fp32, u in [0, 1) (values outside are clamped)
+ *   temperature, top_p, min_p  [R] device fp32, or NULL: 1 / no filter
+ *   top_k        [R] device int32, or NULL
+ *   token, prob  [R] device int32 / fp32, written
+ *   workspace    acceptmoe_sample_workspace_size(R, V) bytes, 256-byte aligned,
+ *                not shared by calls that may run concurrently
+ *   1 <= V <= ACCEPTMOE_MAX_VOCAB, R <= ACCEPTMOE_MAX_SAMPLE_ROWS; R == 0 is a no-op.
+ * Exponentials are taken in 64 bits and summed as whole numbers of 2^-43, so the
+ * result is deterministic and u falls between the borders that 64-bit sums give.
+ */
+size_t acceptmoe_sample_workspace_size(int32_t R, int32_t V);
+int32_t acceptmoe_sample(const void* logits, int32_t dtype, int64_t row_stride, int32_t R, int32_t V,
+                         const float* uniform, const float* temperature, const int32_t* top_k, const float* top_p,
+                         const float* min_p, int32_t* token, float* prob, void* workspace, size_t workspace_bytes,
+                         void* stream);
+
+/*
+ * acceptmoe_accept -- the accepted path of every draft tree, given the target's
+ * token at every node (its argmax or a sample): the tree's first node is on the
+ * path, a later node if its parent is and its token equals target[parent]; of
+ * siblings with the same token the first counts.
+ *   token, parent, target  [T] int32 device; parent holds global node ids (the
+ *                 first node's is ignored); a parent outside the node's tree or
+ *                 not before the node links nothing
+ *   tree_offsets, B  as in acceptmoe_select (HOST array, trees of up to
+ *                 ACCEPTMOE_MAX_TREE_NODES nodes; NULL: one tree)
+ *   on_path       [T] uint8 device, written: 1 on the path, else 0 (what
+ *                 acceptmoe_commit_count takes)
+ *   path          [B, path_len] int32 device, written: the path's global node
+ *                 ids from the root on, then -1; path_len >= the largest tree
+ *   length        [B] int32 device, written: nodes on the path (0: empty tree)
+ *   bonus         [B] int32 device, written: target at the path's last node, the
+ *                 token behind the accepted ones (-1: empty tree)
+ * T == 0 with B == 0 is a no-op.
+ */
+int32_t acceptmoe_accept(const int32_t* token, const int32_t* parent, const int32_t* target,
+                         const int32_t* tree_offsets, int32_t B, int32_t T, uint8_t* on_path, int32_t* path,
+                         int32_t path_len, int32_t* length, int32_t* bonus, void* stream);
 
 /*
  * ---------------------------------------------------------------------------

@@ -34,6 +34,8 @@ MAX_EXPERTS = 512
 MAX_TOPK = 32
 MAX_TREES = 256
 MAX_TREE_NODES = 1024
+MAX_VOCAB = 1 << 20
+MAX_SAMPLE_ROWS = 1 << 20
 SELECT_NOALLOC_MAX_WORKSPACE = 8 << 20
 
 _vp = ctypes.c_void_p
@@ -58,6 +60,11 @@ SIGNATURES = {
     "acceptmoe_moe_forward": (_i32, [_vp, _i32, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp,
                                      _vp, _vp, _sz, _vp]),
     "acceptmoe_residual_add": (_i32, [_vp, _i32, _vp, _i32, _i32, _vp, _vp]),
+    "acceptmoe_residual_norm": (_i32, [_vp, _i32, _vp, _vp, _i32, _i32, ctypes.c_float, _i32, _vp, _vp, _vp, _vp]),
+    "acceptmoe_sample_workspace_size": (_sz, [_i32, _i32]),
+    "acceptmoe_sample": (_i32, [_vp, _i32, ctypes.c_int64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz,
+                                _vp]),
+    "acceptmoe_accept": (_i32, [_vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _vp]),
     "acceptmoe_commit_count": (_i32, [_vp, _vp, _i32, _i32, _vp, _vp]),
     "acceptmoe_commit_estimate": (_i32, [_vp, _vp, _i32, _vp]),
     "acceptmoe_commit_expand": (_i32, [_vp, _i32, _vp, _i32, _vp, _vp]),

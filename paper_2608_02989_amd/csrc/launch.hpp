@@ -95,4 +95,51 @@ size_t forward_workspace_bytes(int T, int H, int I, int E, int k, int is_bf16);
 void forward_carve(void* ws, ForwardParams& p);
 hipError_t launch_forward(ForwardParams p, hipStream_t stream);
 
+// ---- residual norm (norm.hip) ----
+constexpr int kMaxNormWidth = 65536;
+
+struct NormParams {
+  const void* hidden;
+  const float* y;  // addend, may be null
+  const void* weight;
+  void* hidden_out;  // written when y is given
+  void* norm_out;
+  float* scale;
+  int T, H, is_bf16;
+  int group;  // 0: output in the layer's type; else columns per scale, -1: the row
+  float eps;
+};
+hipError_t launch_residual_norm(const NormParams& p, hipStream_t stream);
+
+// ---- accepted path (accept.hip) ----
+struct AcceptParams {
+  const int32_t* token;
+  const int32_t* parent;
+  const int32_t* target;
+  uint8_t* on_path;
+  int32_t* path;
+  int32_t* length;
+  int32_t* bonus;
+  int B, path_len;
+};
+hipError_t launch_accept(const AcceptParams& p, const TreeOffsets& offs, int max_nodes, hipStream_t stream);
+
+// ---- sampling (sample.hip) ----
+constexpr int kMaxVocab = 1 << 20;
+
+struct SampleParams {
+  const void* logits;
+  const float* uniform;
+  const float* temperature;  // this and the filters may be null
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  int32_t* token;
+  float* prob;
+  size_t row_stride;  // elements
+  int R, V, is_bf16;
+};
+size_t sample_workspace_bytes(int R, int V);
+hipError_t launch_sample(const SampleParams& p, hipStream_t stream);
+
 }  // namespace amoe

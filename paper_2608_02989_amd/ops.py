@@ -59,6 +59,14 @@ def _need(t: torch.Tensor, name: str, dtype=None, dim=None):
         raise ValueError(f"{name} must have {dim} dims")
 
 
+def _here(t: torch.Tensor, *others):
+    """All given tensors on the current device: launches go to its streams."""
+    d = torch._C._cuda_getDevice()
+    for x in (t, *others):
+        if x is not None and x.get_device() != d:
+            raise ValueError(f"tensors must be on the current device cuda:{d}, got {x.device}")
+
+
 # ---------------------------------------------------------------------------
 class PackedRouter:
     """Router matrix W_r [E, H] (fp32 as three bf16 planes) in the layout acceptmoe_route reads."""
@@ -341,6 +349,152 @@ def residual_add(hidden: torch.Tensor, y: torch.Tensor, out: torch.Tensor | None
     check(lib().acceptmoe_residual_add(_ptr(hidden), _dtype_code(hidden), _ptr(y), T, H, _ptr(out),
                                        _stream_ptr(stream)))
     return out
+
+
+def residual_norm(hidden: torch.Tensor, y: torch.Tensor | None, weight: torch.Tensor, eps: float = 1e-6,
+                  group: int | None = None, out: dict | None = None, stream=None) -> dict:
+    """hidden + y and its root-mean-square norm (acceptmoe_residual_norm).
+
+    hidden, weight bf16 or fp32, y fp32 or None (no addend: "hidden" is hidden itself).
+    group None: dict(hidden, norm) in hidden's dtype.  group 32, 64, 128 or 256 columns,
+    or -1 for the row: dict(hidden, codes [T, H] float8_e4m3fn, scale [T, H / group] or
+    [T, 1] fp32), codes * scale standing for the norm.  out: such a dict to write into
+    ("hidden" may be hidden itself).
+    """
+    _need(hidden, "hidden", dim=2)
+    _need(weight, "weight", hidden.dtype, 1)
+    T, H = hidden.shape
+    if weight.shape[0] != H:
+        raise ValueError(f"weight must have {H} elements")
+    if y is not None:
+        _need(y, "y", torch.float32, 2)
+        if y.shape != hidden.shape:
+            raise ValueError("residual_norm: hidden and y must have the same shape")
+    code = _dtype_code(hidden)
+    g = 0 if group is None else int(group)
+    if group is not None and g not in (-1, 32, 64, 128, 256):
+        raise ValueError("residual_norm: group must be None, -1, 32, 64, 128 or 256")
+    if g > 0 and H % g != 0:
+        raise ValueError(f"residual_norm: H={H} is no multiple of the group {g}")
+    _here(hidden, y, weight)
+    if out is None:
+        dev = hidden.device
+        res = {"hidden": hidden if y is None else torch.empty_like(hidden)}
+        if g == 0:
+            res["norm"] = torch.empty_like(hidden)
+        else:
+            res["codes"] = torch.empty((T, H), dtype=torch.float8_e4m3fn, device=dev)
+            res["scale"] = torch.empty((T, 1 if g < 0 else H // g), dtype=torch.float32, device=dev)
+    else:
+        res = out
+        want = [("hidden", hidden.dtype, (T, H))] if y is not None else []
+        want += ([("norm", hidden.dtype, (T, H))] if g == 0 else
+                 [("codes", torch.float8_e4m3fn, (T, H)), ("scale", torch.float32, (T, 1 if g < 0 else H // g))])
+        for name, dt, shape in want:
+            _need(res[name], name, dt, 2)
+            if tuple(res[name].shape) != shape:
+                raise ValueError(f"{name} must be {list(shape)}")
+            _here(res[name])
+    check(lib().acceptmoe_residual_norm(
+        hidden.data_ptr(), code, _ptr(y), weight.data_ptr(), T, H, eps, g,
+        None if y is None else res["hidden"].data_ptr(), res["codes" if g else "norm"].data_ptr(),
+        res["scale"].data_ptr() if g else None, _stream_ptr(stream)))
+    return res
+
+
+def sample_workspace(R: int, V: int, device) -> torch.Tensor:
+    """Scratch for sample() on [R, V] logits; calls that may run at the same time need one each."""
+    n = int(lib().acceptmoe_sample_workspace_size(R, V))
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: torch.Tensor | None = None,
+           top_k: torch.Tensor | None = None, top_p: torch.Tensor | None = None, min_p: torch.Tensor | None = None,
+           workspace: torch.Tensor | None = None, outputs: dict | None = None, stream=None) -> dict:
+    """A token per row of logits [R, V] (bf16 or fp32) from the random numbers uniform [R] (acceptmoe_sample).
+
+    temperature, top_p, min_p fp32 [R] and top_k int32 [R], or None; temperature 0: the largest
+    logit.  Rows of logits may be strided (stride(0) >= V).
+    Returns dict(token [R] int32, prob [R] fp32); token -1 where a row has no finite logit.
+    """
+    if not isinstance(logits, torch.Tensor):
+        raise TypeError("logits must be a torch.Tensor")
+    if not logits.is_cuda:
+        raise ValueError("logits must be a device tensor")
+    if logits.dim() != 2:
+        raise ValueError("logits must have 2 dims")
+    R, V = logits.shape
+    step, inner = logits.stride()
+    if (V > 1 and inner != 1) or (R > 1 and step < V):
+        raise ValueError("logits: the tokens of a row must be contiguous and rows must not overlap")
+    code = _dtype_code(logits)
+    _need(uniform, "uniform", torch.float32, 1)
+    for t, name, dt in ((temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32),
+                        (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)):
+        if t is not None:
+            _need(t, name, dt, 1)
+            if t.shape[0] != R:
+                raise ValueError(f"{name} must have {R} elements")
+    if uniform.shape[0] != R:
+        raise ValueError(f"uniform must have {R} elements")
+    _here(logits, uniform, temperature, top_k, top_p, min_p, workspace)
+    dev = logits.device
+    if outputs is None:
+        outputs = {"token": torch.empty(R, dtype=torch.int32, device=dev),
+                   "prob": torch.empty(R, dtype=torch.float32, device=dev)}
+    else:
+        for name, dt in (("token", torch.int32), ("prob", torch.float32)):
+            _need(outputs[name], name, dt, 1)
+            if outputs[name].shape[0] != R:
+                raise ValueError(f"{name} must have {R} elements")
+            _here(outputs[name])
+    if workspace is None:
+        workspace = sample_workspace(R, V, dev)
+    check(lib().acceptmoe_sample(logits.data_ptr(), code, step if R > 1 else V, R, V, uniform.data_ptr(),
+                                 _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
+                                 outputs["token"].data_ptr(), outputs["prob"].data_ptr(), workspace.data_ptr(),
+                                 workspace.numel(), _stream_ptr(stream)))
+    return outputs
+
+
+def accept(token: torch.Tensor, parent: torch.Tensor, target: torch.Tensor, tree_offsets=None,
+           outputs: dict | None = None, stream=None) -> dict:
+    """Accepted path of each draft tree, given the target's token at every node (acceptmoe_accept).
+
+    token, parent, target [T] int32; tree_offsets: host sequence of B+1 ints, or None for one tree.
+    Returns dict(on_path [T] uint8, path [B, nodes of the largest tree] int32 padded with -1,
+    length [B] int32, bonus [B] int32); on_path is what CommitEstimator.add takes.
+    """
+    _need(token, "token", torch.int32, 1)
+    _need(parent, "parent", torch.int32, 1)
+    _need(target, "target", torch.int32, 1)
+    T = token.shape[0]
+    if parent.shape[0] != T or target.shape[0] != T:
+        raise ValueError("accept: token, parent and target must have the same length")
+    _here(token, parent, target)
+    offs_np, offs_ptr, B = _offsets(tree_offsets)  # offs_np: alive until the call returns
+    longest = T if offs_np is None else max(int(np.diff(offs_np).max(initial=0)), 0)
+    if outputs is None:
+        dev = token.device
+        outputs = {"on_path": torch.empty(T, dtype=torch.uint8, device=dev),
+                   "path": torch.empty((B, longest), dtype=torch.int32, device=dev),
+                   "length": torch.empty(B, dtype=torch.int32, device=dev),
+                   "bonus": torch.empty(B, dtype=torch.int32, device=dev)}
+    else:
+        for name, dt, shape in (("on_path", torch.uint8, (T,)), ("length", torch.int32, (B,)),
+                                ("bonus", torch.int32, (B,))):
+            _need(outputs[name], name, dt, 1)
+            if tuple(outputs[name].shape) != shape:
+                raise ValueError(f"{name} must be {list(shape)}")
+        _need(outputs["path"], "path", torch.int32, 2)
+        if outputs["path"].shape[0] != B or outputs["path"].shape[1] < longest:
+            raise ValueError(f"path must be [{B}, >= {longest}]")
+        _here(*outputs.values())
+    path = outputs["path"]
+    check(lib().acceptmoe_accept(token.data_ptr(), parent.data_ptr(), target.data_ptr(), offs_ptr, B, T,
+                                 outputs["on_path"].data_ptr(), path.data_ptr(), path.shape[1],
+                                 outputs["length"].data_ptr(), outputs["bonus"].data_ptr(), _stream_ptr(stream)))
+    return outputs
 
 
 class VerifyStack:

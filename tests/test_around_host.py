@@ -1,0 +1,87 @@
+"""Refusals of the operators around the layer: every call fails its host checks
+before any HIP call (CPU)."""
+import ctypes
+import os
+
+import numpy as np
+import pytest
+
+from paper_2608_02989_amd import _lib as L
+
+pytestmark = pytest.mark.skipif(not os.path.exists(L.LIB_PATH), reason="HIP library not built")
+
+V = ctypes.c_void_p
+A, B, C, D, E = (V(0x100000 + i * 0x10000000) for i in range(5))  # aligned, apart, never dereferenced
+
+
+def refused(rc, code, word):
+    assert rc == code and word in L.lib().acceptmoe_last_error().decode()
+
+
+def norm(hidden=A, dtype=L.BF16, y=B, weight=C, T=4, H=64, eps=1e-6, group=0, hidden_out=A, norm_out=D, scale=E):
+    return L.lib().acceptmoe_residual_norm(hidden, dtype, y, weight, T, H, eps, group, hidden_out, norm_out, scale, None)
+
+
+@pytest.mark.parametrize("change,code,word", [
+    ({"dtype": 7}, L.ERR_INVALID_ARG, "dtype"), ({"T": -1}, L.ERR_INVALID_ARG, "sizes"),
+    ({"H": 0}, L.ERR_INVALID_ARG, "sizes"), ({"H": 66}, L.ERR_UNSUPPORTED, "multiple of 4"),
+    ({"H": 65540}, L.ERR_UNSUPPORTED, "65536"), ({"eps": -1.0}, L.ERR_INVALID_ARG, "eps"),
+    ({"eps": float("nan")}, L.ERR_INVALID_ARG, "eps"), ({"group": 48}, L.ERR_UNSUPPORTED, "group"),
+    ({"group": 128}, L.ERR_UNSUPPORTED, "multiple of the group"), ({"hidden": None}, L.ERR_INVALID_ARG, "null"),
+    ({"weight": None}, L.ERR_INVALID_ARG, "null"), ({"norm_out": None}, L.ERR_INVALID_ARG, "null"),
+    ({"hidden_out": None}, L.ERR_INVALID_ARG, "hidden_out"), ({"group": 32, "scale": None}, L.ERR_INVALID_ARG, "scale"),
+    ({"y": V(0x100008)}, L.ERR_INVALID_ARG, "aligned"), ({"norm_out": A}, L.ERR_INVALID_ARG, "overlaps"),
+    ({"hidden_out": V(0x100010)}, L.ERR_INVALID_ARG, "overlaps"), ({"hidden_out": D}, L.ERR_INVALID_ARG, "overlaps")])
+def test_residual_norm_rejects(change, code, word):
+    refused(norm(**change), code, word)
+
+
+def test_no_ops():
+    assert norm(T=0) == L.OK
+    assert sample(R=0) == L.OK
+    assert accept(T=0, trees=0) == L.OK
+
+
+def sample(logits=A, dtype=L.F32, stride=100, R=2, vocab=100, u=B, token=C, prob=D, ws=E, nbytes=1 << 30):
+    return L.lib().acceptmoe_sample(logits, dtype, stride, R, vocab, u, None, None, None, None, token, prob, ws, nbytes,
+                                    None)
+
+
+@pytest.mark.parametrize("change,code,word", [
+    ({"dtype": 2}, L.ERR_INVALID_ARG, "dtype"), ({"R": -1}, L.ERR_INVALID_ARG, "sizes"),
+    ({"vocab": 0}, L.ERR_INVALID_ARG, "sizes"), ({"vocab": L.MAX_VOCAB + 1, "stride": 1 << 21}, L.ERR_UNSUPPORTED, "V must"),
+    ({"R": L.MAX_SAMPLE_ROWS + 1}, L.ERR_UNSUPPORTED, "R <="), ({"stride": 99}, L.ERR_INVALID_ARG, "row_stride"),
+    ({"logits": None}, L.ERR_INVALID_ARG, "null"), ({"u": None}, L.ERR_INVALID_ARG, "null"),
+    ({"token": None}, L.ERR_INVALID_ARG, "null"), ({"prob": None}, L.ERR_INVALID_ARG, "null"),
+    ({"logits": V(0x100002)}, L.ERR_INVALID_ARG, "aligned"), ({"ws": None}, L.ERR_WORKSPACE, "workspace"),
+    ({"nbytes": 0}, L.ERR_WORKSPACE, "workspace"), ({"ws": V(0x100010)}, L.ERR_WORKSPACE, "aligned")])
+def test_sample_rejects(change, code, word):
+    refused(sample(**change), code, word)
+
+
+def test_sample_workspace_size():
+    f = L.lib().acceptmoe_sample_workspace_size
+    assert f(4, 0) == 0 and f(-1, 10) == 0 and f(4, L.MAX_VOCAB + 1) == 0
+    for vocab in (1, 1000, 32000, 131072, L.MAX_VOCAB):
+        sizes = [f(r, vocab) for r in range(0, 600)]
+        assert sizes == sorted(sizes) and sizes[1] > 0
+
+
+def accept(token=A, parent=B, target=C, offs=None, trees=1, T=5, on=D, path=E, path_len=5, length=A, bonus=B):
+    arr = None if offs is None else np.ascontiguousarray(offs, np.int32)
+    return L.lib().acceptmoe_accept(token, parent, target, None if arr is None else arr.ctypes.data, trees, T, on, path,
+                                    path_len, length, bonus, None)
+
+
+@pytest.mark.parametrize("change,code,word", [
+    ({"T": -1}, L.ERR_INVALID_ARG, "T must"), ({"trees": 0}, L.ERR_UNSUPPORTED, "B must"),
+    ({"trees": 257}, L.ERR_UNSUPPORTED, "B must"), ({"trees": 2}, L.ERR_INVALID_ARG, "NULL"),
+    ({"offs": [1, 5]}, L.ERR_INVALID_ARG, "must be 0"), ({"offs": [0, 4]}, L.ERR_INVALID_ARG, "equal T"),
+    ({"offs": [0, 7, 5], "trees": 2}, L.ERR_INVALID_ARG, "non-decreasing"),
+    ({"T": 1025, "path_len": 1025}, L.ERR_UNSUPPORTED, "nodes"), ({"path_len": 4}, L.ERR_INVALID_ARG, "path_len"),
+    ({"token": None}, L.ERR_INVALID_ARG, "null"), ({"parent": None}, L.ERR_INVALID_ARG, "null"),
+    ({"target": None}, L.ERR_INVALID_ARG, "null"), ({"on": None}, L.ERR_INVALID_ARG, "null"),
+    ({"path": None}, L.ERR_INVALID_ARG, "null"), ({"length": None}, L.ERR_INVALID_ARG, "null"),
+    ({"bonus": None}, L.ERR_INVALID_ARG, "null")])
+def test_accept_rejects(change, code, word):
+    refused(accept(**change), code, word)
