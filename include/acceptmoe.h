@@ -287,6 +287,48 @@ int32_t acceptmoe_moe_forward(const void* hidden, int32_t dtype, const void* w_g
                               size_t workspace_bytes, void* stream);
 
 /*
+ * ---------------------------------------------------------------------------
+ * Experts with weights in 4 bits
+ * ---------------------------------------------------------------------------
+ * A weight is an e2m1 code (sign, 2 exponent bits, 1 mantissa bit: 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 for codes 0 .. 7, their negatives for 8 .. 15) times a power
+ * of two shared by 32 neighbouring columns of its row, held as a byte s:
+ *   W = code * 2^(s - 127),  2 <= s <= 252 (others: unspecified).
+ * A stack [E, N, K] is two arrays: codes [E, N, K / 2] uint8, two a byte, the
+ * lower nibble the column before, and scales [E, N, K / 32] uint8.
+ *
+ * acceptmoe_quantize_q4 -- codes and scales of n values (n % 32 == 0; any row
+ * length that is a multiple of 32): per 32 neighbours the smallest scale that holds
+ * their largest magnitude within 6 of it (s between 2 and 252), every value to the
+ * nearest code, ties to the even one.  w F32 or BF16, finite.
+ * acceptmoe_pack_gate_up_q4, acceptmoe_pack_down_q4 -- the layouts that
+ * acceptmoe_moe_forward_q4 reads.  Per expert and quad of 16-row tiles (gate 2p,
+ * gate 2p + 1, up 2p, up 2p + 1; four tiles of W_d), and per 128 columns: four
+ * fragments of 64 lanes x 16 B, lane L holding the codes of row L % 16, columns
+ * 32 * (L / 16) .. + 31, then 64 lanes x 4 B with the four fragments' scales.
+ * Rows and columns past the stack are zeros.  acceptmoe_q4_gate_up_bytes and
+ * acceptmoe_q4_down_bytes give the sizes (0 for unsupported ones).
+ * acceptmoe_moe_forward_q4 -- acceptmoe_moe_forward over such weights: hidden
+ * [T, H] bf16, the same routing, out [T, H] fp32.  The products of the gate and up
+ * projections are exact with fp32 accumulation; the activation goes to the down
+ * projection in 16 significant bits (as two bf16 numbers).  Deterministic.
+ *   H and I positive multiples of 32 up to 65536, 1 <= E <= ACCEPTMOE_MAX_EXPERTS,
+ *   1 <= k <= ACCEPTMOE_MAX_TOPK; T == 0 is a no-op.  workspace as for
+ *   acceptmoe_moe_forward, of acceptmoe_moe_forward_q4_workspace_size bytes.
+ */
+size_t acceptmoe_q4_gate_up_bytes(int32_t E, int32_t I, int32_t H);
+size_t acceptmoe_q4_down_bytes(int32_t E, int32_t H, int32_t I);
+int32_t acceptmoe_quantize_q4(const void* w, int32_t dtype, int64_t n, uint8_t* codes, uint8_t* scales, void* stream);
+int32_t acceptmoe_pack_gate_up_q4(const uint8_t* gate, const uint8_t* gate_scale, const uint8_t* up,
+                                  const uint8_t* up_scale, int32_t E, int32_t I, int32_t H, void* dst, void* stream);
+int32_t acceptmoe_pack_down_q4(const uint8_t* down, const uint8_t* down_scale, int32_t E, int32_t H, int32_t I,
+                               void* dst, void* stream);
+size_t acceptmoe_moe_forward_q4_workspace_size(int32_t T, int32_t H, int32_t I, int32_t E, int32_t k);
+int32_t acceptmoe_moe_forward_q4(const void* hidden, const void* w_gate_up, const void* w_down, int32_t T, int32_t H,
+                                 int32_t I, int32_t E, int32_t k, const int32_t* topk_idx, const float* topk_gate,
+                                 float* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * acceptmoe_residual_add -- out = hidden + y, rounded to `dtype` (bf16: the
  * fp32 sum rounded to nearest even; fp32: the plain sum).  Chains stacked
  * verify layers: the next layer's input is the previous one's input plus its

@@ -77,3 +77,48 @@ def accept(token, parent, target, offsets):
         length.append(len(walk))
         bonus.append(int(target[walk[-1]]) if walk else -1)
     return on, paths, length, bonus
+
+
+E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, -0.0, -0.5, -1.0, -1.5, -2.0, -3.0, -4.0, -6.0])
+
+
+def dequantize_q4(codes, scales):
+    """[..., K / 2] codes (lower nibble first) and [..., K / 32] scales -> [..., K] fp64."""
+    codes, scales = np.asarray(codes), np.asarray(scales)
+    v = E2M1[np.stack([codes & 15, codes >> 4], axis=-1)].reshape(*codes.shape[:-1], -1)
+    return v * np.repeat(2.0 ** (scales.astype(np.float64) - 127), 32, axis=-1)
+
+
+def quantize_q4(w):
+    """Codes and scales of [..., K]: the smallest scale with max|w| <= 6 of it, nearest code, ties to even."""
+    w = np.asarray(w, np.float64)
+    parts = w.reshape(*w.shape[:-1], -1, 32)
+    largest = np.abs(parts).max(axis=-1)
+    scales = np.full(largest.shape, 2, np.int64)
+    for s in range(251, 1, -1):
+        scales[largest > 6 * 2.0 ** (s - 127)] = np.maximum(scales[largest > 6 * 2.0 ** (s - 127)], s + 1)
+    a = np.abs(parts) / 2.0 ** (scales[..., None] - 127.0)
+    dist = np.abs(a[..., None] - E2M1[:8])
+    nearest = dist.min(axis=-1, keepdims=True) == dist
+    # of two equally near neighbours the even code
+    code = np.where(nearest.sum(axis=-1) == 2, np.argmax(nearest & (np.arange(8) % 2 == 0), axis=-1),
+                    np.argmax(nearest, axis=-1))
+    code = (code + 8 * np.signbit(parts)).reshape(w.shape).astype(np.uint8)
+    return code[..., 0::2] | (code[..., 1::2] << 4), scales.astype(np.uint8)
+
+
+def moe_forward(x, gate, up, down, idx, g):
+    """Grouped SwiGLU FFN in fp64; gate, up [E, I, H], down [E, H, I]; routing entries outside
+    [0, E) are skipped and a repeated expert counts at its first slot."""
+    x = np.asarray(x, np.float64)
+    out = np.zeros_like(x)
+    for t, row in enumerate(idx):
+        seen = set()
+        for j, e in enumerate(row):
+            if not 0 <= e < len(gate) or e in seen:
+                continue
+            seen.add(e)
+            z = gate[e] @ x[t]
+            with np.errstate(over="ignore"):
+                out[t] += g[t][j] * (down[e] @ (z / (1 + np.exp(-z)) * (up[e] @ x[t])))
+    return out

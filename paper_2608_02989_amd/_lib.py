@@ -59,6 +59,13 @@ SIGNATURES = {
     "acceptmoe_pack_gate_up_weights": (_i32, [_vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp]),
     "acceptmoe_moe_forward": (_i32, [_vp, _i32, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp,
                                      _vp, _vp, _sz, _vp]),
+    "acceptmoe_q4_gate_up_bytes": (_sz, [_i32, _i32, _i32]),
+    "acceptmoe_q4_down_bytes": (_sz, [_i32, _i32, _i32]),
+    "acceptmoe_quantize_q4": (_i32, [_vp, _i32, ctypes.c_int64, _vp, _vp, _vp]),
+    "acceptmoe_pack_gate_up_q4": (_i32, [_vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp]),
+    "acceptmoe_pack_down_q4": (_i32, [_vp, _vp, _i32, _i32, _i32, _vp, _vp]),
+    "acceptmoe_moe_forward_q4_workspace_size": (_sz, [_i32, _i32, _i32, _i32, _i32]),
+    "acceptmoe_moe_forward_q4": (_i32, [_vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
     "acceptmoe_residual_add": (_i32, [_vp, _i32, _vp, _i32, _i32, _vp, _vp]),
     "acceptmoe_residual_norm": (_i32, [_vp, _i32, _vp, _vp, _i32, _i32, ctypes.c_float, _i32, _vp, _vp, _vp, _vp]),
     "acceptmoe_sample_workspace_size": (_sz, [_i32, _i32]),

@@ -1,5 +1,5 @@
 // C ABI of the operators around the layer (residual norm, sampling,
-// accepted path): host-side argument checks (before any HIP call) and kernel
+// accepted path) and of the experts with 4-bit weights: host-side argument checks (before any HIP call) and kernel
 // launches.  See include/acceptmoe.h.
 #include "acceptmoe.h"
 
@@ -23,6 +23,19 @@ bool overlap(const void* a, size_t an, const void* b, size_t bn) {
   const char* x = static_cast<const char*>(a);
   const char* y = static_cast<const char*>(b);
   return x < y + bn && y < x + an;
+}
+
+constexpr int kQ4MaxSize = 65536;  // a quad's run over K stays addressable by 32 bits
+
+bool q4_size(int32_t n) { return n >= 32 && n % 32 == 0 && n <= kQ4MaxSize; }
+
+int32_t q4_check(const char* who, int32_t E, int32_t I, int32_t H) {
+  if (E < 1 || E > ACCEPTMOE_MAX_EXPERTS)
+    return fail(ACCEPTMOE_ERR_UNSUPPORTED, "%s: E must be in [1, %d] (got %d)", who, ACCEPTMOE_MAX_EXPERTS, E);
+  if (!q4_size(H) || !q4_size(I))
+    return fail(ACCEPTMOE_ERR_UNSUPPORTED, "%s: H and I must be positive multiples of 32 up to %d (H=%d I=%d)", who,
+                kQ4MaxSize, H, I);
+  return ACCEPTMOE_OK;
 }
 
 }  // namespace
@@ -148,6 +161,115 @@ int32_t acceptmoe_accept(const int32_t* token, const int32_t* parent, const int3
   const amoe::AcceptParams p = {token, parent, target, on_path, path, length, bonus, B, path_len};
   hipError_t e = amoe::launch_accept(p, offs, longest, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ACCEPTMOE_OK : hip_fail(e, "accept launch");
+}
+
+// ---------------------------------------------------------------------------
+size_t acceptmoe_q4_gate_up_bytes(int32_t E, int32_t I, int32_t H) {
+  if (E < 1 || E > ACCEPTMOE_MAX_EXPERTS || !q4_size(I) || !q4_size(H)) return 0;
+  return amoe::packed_gate_up_q4_bytes(E, I, H);
+}
+
+size_t acceptmoe_q4_down_bytes(int32_t E, int32_t H, int32_t I) {
+  if (E < 1 || E > ACCEPTMOE_MAX_EXPERTS || !q4_size(I) || !q4_size(H)) return 0;
+  return amoe::packed_down_q4_bytes(E, H, I);
+}
+
+int32_t acceptmoe_quantize_q4(const void* w, int32_t dtype, int64_t n, uint8_t* codes, uint8_t* scales, void* stream) {
+  clear_err();
+  if (dtype != ACCEPTMOE_F32 && dtype != ACCEPTMOE_BF16)
+    return fail(ACCEPTMOE_ERR_INVALID_ARG, "quantize_q4: unknown dtype %d", dtype);
+  if (n < 0 || n % 32 != 0)
+    return fail(ACCEPTMOE_ERR_INVALID_ARG, "quantize_q4: n must be a multiple of 32 (got %lld)",
+                static_cast<long long>(n));
+  if (n == 0) return ACCEPTMOE_OK;
+  if (!w || !codes || !scales) return fail(ACCEPTMOE_ERR_INVALID_ARG, "quantize_q4: null pointer");
+  if (!aligned(w, 16) || !aligned(codes, 16))
+    return fail(ACCEPTMOE_ERR_INVALID_ARG, "quantize_q4: w and codes must be 16-byte aligned");
+  const size_t bytes = static_cast<size_t>(n) * (dtype == ACCEPTMOE_BF16 ? 2 : 4);
+  if (overlap(w, bytes, codes, n / 2) || overlap(w, bytes, scales, n / 32) || overlap(codes, n / 2, scales, n / 32))
+    return fail(ACCEPTMOE_ERR_INVALID_ARG, "quantize_q4: arguments overlap");
+  hipError_t e = amoe::launch_quantize_q4(w, dtype == ACCEPTMOE_BF16, static_cast<size_t>(n) / 32, codes, scales,
+                                          static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ACCEPTMOE_OK : hip_fail(e, "quantize_q4 launch");
+}
+
+int32_t acceptmoe_pack_gate_up_q4(const uint8_t* gate, const uint8_t* gate_scale, const uint8_t* up,
+                                  const uint8_t* up_scale, int32_t E, int32_t I, int32_t H, void* dst, void* stream) {
+  clear_err();
+  const int32_t rc = q4_check("pack_gate_up_q4", E, I, H);
+  if (rc != ACCEPTMOE_OK) return rc;
+  if (!gate || !gate_scale || !up || !up_scale || !dst)
+    return fail(ACCEPTMOE_ERR_INVALID_ARG, "pack_gate_up_q4: null pointer");
+  if (!aligned(gate, 16) || !aligned(up, 16) || !aligned(dst, 16))
+    return fail(ACCEPTMOE_ERR_INVALID_ARG, "pack_gate_up_q4: codes and dst must be 16-byte aligned");
+  const size_t n = static_cast<size_t>(E) * I * H, out = amoe::packed_gate_up_q4_bytes(E, I, H);
+  if (overlap(dst, out, gate, n / 2) || overlap(dst, out, up, n / 2) || overlap(dst, out, gate_scale, n / 32) ||
+      overlap(dst, out, up_scale, n / 32))
+    return fail(ACCEPTMOE_ERR_INVALID_ARG, "pack_gate_up_q4: a source overlaps dst");
+  hipError_t e = amoe::launch_pack_gate_up_q4(gate, gate_scale, up, up_scale, E, I, H, dst,
+                                              static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ACCEPTMOE_OK : hip_fail(e, "pack_gate_up_q4 launch");
+}
+
+int32_t acceptmoe_pack_down_q4(const uint8_t* down, const uint8_t* down_scale, int32_t E, int32_t H, int32_t I,
+                               void* dst, void* stream) {
+  clear_err();
+  const int32_t rc = q4_check("pack_down_q4", E, I, H);
+  if (rc != ACCEPTMOE_OK) return rc;
+  if (!down || !down_scale || !dst) return fail(ACCEPTMOE_ERR_INVALID_ARG, "pack_down_q4: null pointer");
+  if (!aligned(down, 16) || !aligned(dst, 16))
+    return fail(ACCEPTMOE_ERR_INVALID_ARG, "pack_down_q4: codes and dst must be 16-byte aligned");
+  const size_t n = static_cast<size_t>(E) * I * H, out = amoe::packed_down_q4_bytes(E, H, I);
+  if (overlap(dst, out, down, n / 2) || overlap(dst, out, down_scale, n / 32))
+    return fail(ACCEPTMOE_ERR_INVALID_ARG, "pack_down_q4: a source overlaps dst");
+  hipError_t e = amoe::launch_pack_down_q4(down, down_scale, E, H, I, dst, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ACCEPTMOE_OK : hip_fail(e, "pack_down_q4 launch");
+}
+
+size_t acceptmoe_moe_forward_q4_workspace_size(int32_t T, int32_t H, int32_t I, int32_t E, int32_t k) {
+  if (T < 0 || H < 1 || I < 1 || E < 1 || k < 1) return 0;
+  return amoe::forward_q4_workspace_bytes(T, H, I, E, k);
+}
+
+int32_t acceptmoe_moe_forward_q4(const void* hidden, const void* w_gate_up, const void* w_down, int32_t T, int32_t H,
+                                 int32_t I, int32_t E, int32_t k, const int32_t* topk_idx, const float* topk_gate,
+                                 float* out, void* workspace, size_t workspace_bytes, void* stream) {
+  clear_err();
+  if (T < 0) return fail(ACCEPTMOE_ERR_INVALID_ARG, "forward_q4: T must be >= 0 (got %d)", T);
+  const int32_t rc = q4_check("forward_q4", E, I, H);
+  if (rc != ACCEPTMOE_OK) return rc;
+  if (k < 1 || k > ACCEPTMOE_MAX_TOPK)
+    return fail(ACCEPTMOE_ERR_UNSUPPORTED, "forward_q4: k must be in [1, %d] (got %d)", ACCEPTMOE_MAX_TOPK, k);
+  if (T == 0) return ACCEPTMOE_OK;
+  if (static_cast<long long>(T) * k > (1ll << 30)) return fail(ACCEPTMOE_ERR_UNSUPPORTED, "forward_q4: T*k too large");
+  if (static_cast<long long>((H / 4 + 255) / 256) * T >= (1ll << 31))
+    return fail(ACCEPTMOE_ERR_UNSUPPORTED, "forward_q4: T * ceil(H / 1024) must stay below 2^31 (T=%d H=%d)", T, H);
+  if (!hidden || !w_gate_up || !w_down || !topk_idx || !topk_gate || !out)
+    return fail(ACCEPTMOE_ERR_INVALID_ARG, "forward_q4: null pointer");
+  if (!aligned(hidden, 16) || !aligned(w_gate_up, 16) || !aligned(w_down, 16) || !aligned(out, 16))
+    return fail(ACCEPTMOE_ERR_INVALID_ARG, "forward_q4: hidden, weights and out must be 16-byte aligned");
+  const size_t need = amoe::forward_q4_workspace_bytes(T, H, I, E, k);
+  if (workspace == nullptr || workspace_bytes < need)
+    return fail(ACCEPTMOE_ERR_WORKSPACE, "forward_q4: workspace needs %zu bytes (got %zu)", need, workspace_bytes);
+  if (!aligned(workspace, 256))
+    return fail(ACCEPTMOE_ERR_WORKSPACE, "forward_q4: workspace must be 256-byte aligned");
+  amoe::ForwardParams p;
+  std::memset(&p, 0, sizeof p);
+  p.hidden = hidden;
+  p.w_gate_up = w_gate_up;
+  p.w_down = w_down;
+  p.topk_idx = topk_idx;
+  p.topk_gate = topk_gate;
+  p.out = out;
+  p.T = T;
+  p.H = H;
+  p.I = I;
+  p.E = E;
+  p.k = k;
+  p.is_bf16 = 1;
+  amoe::forward_q4_carve(workspace, p);
+  hipError_t e = amoe::launch_forward_q4(p, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ACCEPTMOE_OK : hip_fail(e, "forward_q4 launch");
 }
 
 }  // extern "C"

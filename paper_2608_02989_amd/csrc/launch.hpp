@@ -142,4 +142,17 @@ struct SampleParams {
 size_t sample_workspace_bytes(int R, int V);
 hipError_t launch_sample(const SampleParams& p, hipStream_t stream);
 
+// ---- expert FFN with 4-bit weights (q4.hip) ----
+size_t packed_gate_up_q4_bytes(int E, int I, int H);
+size_t packed_down_q4_bytes(int E, int H, int I);
+hipError_t launch_pack_gate_up_q4(const uint8_t* gate, const uint8_t* gate_scale, const uint8_t* up,
+                                  const uint8_t* up_scale, int E, int I, int H, void* dst, hipStream_t stream);
+hipError_t launch_pack_down_q4(const uint8_t* down, const uint8_t* down_scale, int E, int H, int I, void* dst,
+                               hipStream_t stream);
+hipError_t launch_quantize_q4(const void* w, int is_bf16, size_t groups, uint8_t* codes, uint8_t* scales,
+                              hipStream_t stream);
+size_t forward_q4_workspace_bytes(int T, int H, int I, int E, int k);
+void forward_q4_carve(void* ws, ForwardParams& p);
+hipError_t launch_forward_q4(const ForwardParams& p, hipStream_t stream);
+
 }  // namespace amoe

@@ -244,6 +244,115 @@ def moe_forward(hidden: torch.Tensor, w_gate_up: PackedGateUp, w_down_p: torch.T
 
 
 # ---------------------------------------------------------------------------
+# experts with weights in 4 bits (e2m1 codes, a power of two per 32 columns)
+# ---------------------------------------------------------------------------
+Q4_GROUP = 32
+
+
+def quantize_q4(w: torch.Tensor, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+    """Stack [..., K] (bf16 or fp32, K % 32 == 0) -> (codes [..., K / 2], scales [..., K / 32]), both uint8
+    (acceptmoe_quantize_q4)."""
+    _need(w, "w")
+    if w.dim() < 1 or w.shape[-1] % Q4_GROUP != 0:
+        raise ValueError(f"quantize_q4: the last dimension must be a multiple of {Q4_GROUP}, got {tuple(w.shape)}")
+    _here(w)
+    K = w.shape[-1]
+    codes = torch.empty((*w.shape[:-1], K // 2), dtype=torch.uint8, device=w.device)
+    scales = torch.empty((*w.shape[:-1], K // Q4_GROUP), dtype=torch.uint8, device=w.device)
+    check(lib().acceptmoe_quantize_q4(_ptr(w), _dtype_code(w), w.numel(), _ptr(codes), _ptr(scales), _stream_ptr(stream)))
+    return codes, scales
+
+
+class PackedQ4:
+    """A 4-bit weight stack in the layout acceptmoe_moe_forward_q4 reads: "gate_up" (N = I,
+    K = H) or "down" (N = H, K = I)."""
+
+    def __init__(self, data: torch.Tensor, kind: str, E: int, N: int, K: int):
+        self.data, self.kind, self.E, self.N, self.K = data, kind, E, N, K
+
+
+def _need_q4(codes, scales, name):
+    _need(codes, name, torch.uint8, 3)
+    _need(scales, f"{name}_scale", torch.uint8, 3)
+    E, N, half = codes.shape
+    if half % 16 != 0 or tuple(scales.shape) != (E, N, half // 16):
+        raise ValueError(f"{name}: codes [E, N, K / 2] need scales [E, N, K / {Q4_GROUP}], "
+                         f"got {tuple(codes.shape)} and {tuple(scales.shape)}")
+    _here(codes, scales)
+    return E, N, 2 * half
+
+
+def pack_gate_up_q4(gate: torch.Tensor, gate_scale: torch.Tensor, up: torch.Tensor, up_scale: torch.Tensor,
+                    stream=None) -> PackedQ4:
+    """Gate and up stacks [E, I, H] as codes and scales -> one PackedQ4 (acceptmoe_pack_gate_up_q4)."""
+    E, I, H = _need_q4(gate, gate_scale, "gate")
+    if _need_q4(up, up_scale, "up") != (E, I, H):
+        raise ValueError("gate and up must have the same shape")
+    n = int(lib().acceptmoe_q4_gate_up_bytes(E, I, H))
+    if n == 0:
+        raise ValueError(f"unsupported gate/up shape E={E} I={I} H={H}")
+    data = torch.empty(n, dtype=torch.uint8, device=gate.device)
+    check(lib().acceptmoe_pack_gate_up_q4(_ptr(gate), _ptr(gate_scale), _ptr(up), _ptr(up_scale), E, I, H, _ptr(data),
+                                          _stream_ptr(stream)))
+    return PackedQ4(data, "gate_up", E, I, H)
+
+
+def pack_down_q4(down: torch.Tensor, down_scale: torch.Tensor, stream=None) -> PackedQ4:
+    """Down stack [E, H, I] as codes and scales -> PackedQ4 (acceptmoe_pack_down_q4)."""
+    E, H, I = _need_q4(down, down_scale, "down")
+    n = int(lib().acceptmoe_q4_down_bytes(E, H, I))
+    if n == 0:
+        raise ValueError(f"unsupported down shape E={E} H={H} I={I}")
+    data = torch.empty(n, dtype=torch.uint8, device=down.device)
+    check(lib().acceptmoe_pack_down_q4(_ptr(down), _ptr(down_scale), E, H, I, _ptr(data), _stream_ptr(stream)))
+    return PackedQ4(data, "down", E, H, I)
+
+
+def forward_q4_workspace(T: int, H: int, I: int, E: int, k: int, device) -> torch.Tensor:
+    n = lib().acceptmoe_moe_forward_q4_workspace_size(T, H, I, E, k)
+    return torch.empty(max(int(n), 256), dtype=torch.uint8, device=device)
+
+
+def _need_packed_q4(w_gate_up, w_down):
+    if not isinstance(w_gate_up, PackedQ4) or w_gate_up.kind != "gate_up":
+        raise TypeError("w_gate_up must come from pack_gate_up_q4")
+    if not isinstance(w_down, PackedQ4) or w_down.kind != "down":
+        raise TypeError("w_down must come from pack_down_q4")
+    if (w_down.E, w_down.N, w_down.K) != (w_gate_up.E, w_gate_up.K, w_gate_up.N):
+        raise ValueError("weights must be gate/up packed from [E, I, H] stacks and down [E, H, I]")
+
+
+def moe_forward_q4(hidden: torch.Tensor, w_gate_up: PackedQ4, w_down: PackedQ4, topk_idx: torch.Tensor,
+                   topk_gate: torch.Tensor, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                   stream=None) -> torch.Tensor:
+    """Grouped SwiGLU expert FFN over 4-bit weights (acceptmoe_moe_forward_q4): hidden [T, H] bf16 -> [T, H] fp32."""
+    _need(hidden, "hidden", torch.bfloat16, 2)
+    _need_packed_q4(w_gate_up, w_down)
+    _need(topk_idx, "topk_idx", torch.int32, 2)
+    _need(topk_gate, "topk_gate", torch.float32, 2)
+    T, H = hidden.shape
+    E, I = w_gate_up.E, w_gate_up.N
+    k = topk_idx.shape[1]
+    if w_gate_up.K != H:
+        raise ValueError(f"weights packed for H={w_gate_up.K}, hidden has H={H}")
+    if topk_idx.shape[0] != T or topk_gate.shape != topk_idx.shape:
+        raise ValueError("topk_idx / topk_gate must be [T, k]")
+    _here(hidden, w_gate_up.data, w_down.data, topk_idx, topk_gate, out, workspace)
+    if out is None:
+        out = torch.empty((T, H), dtype=torch.float32, device=hidden.device)
+    else:
+        _need(out, "out", torch.float32, 2)
+        if out.shape != hidden.shape:
+            raise ValueError("out must be [T, H]")
+    if workspace is None:
+        workspace = forward_q4_workspace(T, H, I, E, k, hidden.device)
+    check(lib().acceptmoe_moe_forward_q4(
+        hidden.data_ptr(), w_gate_up.data.data_ptr(), w_down.data.data_ptr(), T, H, I, E, k, topk_idx.data_ptr(),
+        topk_gate.data_ptr(), out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
+    return out
+
+
+# ---------------------------------------------------------------------------
 class VerifyLayer:
     """One MoE layer with packed expert weights and preallocated workspaces.
 
@@ -268,7 +377,7 @@ class VerifyLayer:
         self.max_tokens, self.max_trees = max_tokens, max_trees
         self.logits = torch.empty((T, self.E), dtype=torch.float32, device=dev)
         self.sel_ws = select_workspace(T, self.E, k, dev)
-        self.fwd_ws = forward_workspace(T, self.H, self.I, self.E, k, self.dtype, dev)
+        self.fwd_ws = self._forward_workspace(T, dev)
         self.sel_out = {
             "eligible": torch.empty((max_trees, self.E), dtype=torch.uint8, device=dev),
             "idx": torch.empty((T, k), dtype=torch.int32, device=dev),
@@ -276,6 +385,9 @@ class VerifyLayer:
             "stats": torch.empty((max_trees, L.NUM_STATS), dtype=torch.int32, device=dev),
         }
         self.out = torch.empty((T, self.H), dtype=torch.float32, device=dev)
+
+    def _forward_workspace(self, T: int, dev) -> torch.Tensor:
+        return forward_workspace(T, self.H, self.I, self.E, self.k, self.dtype, dev)
 
     def twin(self) -> "VerifyLayer":
         """The same layer (shared packed weights) with its own workspaces and
@@ -336,6 +448,45 @@ class VerifyLayer:
                              "stats": buf["stats"][:B]}, out[:T])
 
 
+class VerifyLayerQ4(VerifyLayer):
+    """VerifyLayer whose experts are held in 4 bits.  w_gate, w_up [E, I, H] and w_down
+    [E, H, I] are quantised here (bf16 or fp32 stacks), or given as (codes, scales) pairs.
+    The hidden states are bf16."""
+
+    def __init__(self, router_w: torch.Tensor, w_gate, w_up, w_down, k: int, max_tokens: int, max_trees: int = 1,
+                 beta: float = 0.5, mode: int = L.MODE_SELF_SIZING, budget: int = 0, removal_cap: int = -1):
+        pairs = [quantize_q4(w) if isinstance(w, torch.Tensor) else w for w in (w_gate, w_up, w_down)]
+        self.router_w = router_w
+        self.router = pack_router_weights(router_w)
+        self.wgu = pack_gate_up_q4(*pairs[0], *pairs[1])
+        self.wd = pack_down_q4(*pairs[2])
+        _need_packed_q4(self.wgu, self.wd)
+        self.E, self.I, self.H = self.wgu.E, self.wgu.N, self.wgu.K
+        if self.router.E != self.E or self.router.H != self.H:
+            raise ValueError(f"router_w must be [{self.E}, {self.H}], got {tuple(router_w.shape)}")
+        self.k, self.beta, self.mode, self.budget, self.removal_cap = k, beta, mode, budget, removal_cap
+        self.dtype = torch.bfloat16
+        self._alloc(max_tokens, max_trees, router_w.device)
+
+    def _forward_workspace(self, T: int, dev) -> torch.Tensor:
+        return forward_q4_workspace(T, self.H, self.I, self.E, self.k, dev)
+
+    def step(self, hidden, parent, depth, prob, tree_offsets=None, resident=None, stream=None):
+        _need(hidden, "hidden", torch.bfloat16, 2)
+        T = hidden.shape[0]
+        B = 1 if tree_offsets is None else len(tree_offsets) - 1
+        if T > self.max_tokens or B > self.max_trees:
+            raise ValueError(f"layer holds {self.max_tokens} tokens in {self.max_trees} trees, got {T} in {B}")
+        buf = self.sel_out
+        outs = {"eligible": buf["eligible"][:B], "idx": buf["idx"][:T], "gate": buf["gate"][:T], "stats": buf["stats"][:B]}
+        logits, out = self.logits[:T], self.out[:T]
+        route(hidden, self.router, out=logits, stream=stream)
+        select(logits, parent, depth, prob, tree_offsets, self.k, self.beta, self.mode, self.budget, self.removal_cap,
+               resident, workspace=self.sel_ws, outputs=outs, stream=stream)
+        moe_forward_q4(hidden, self.wgu, self.wd, outs["idx"], outs["gate"], out=out, workspace=self.fwd_ws, stream=stream)
+        return logits, outs, out
+
+
 def residual_add(hidden: torch.Tensor, y: torch.Tensor, out: torch.Tensor | None = None,
                  stream=None) -> torch.Tensor:
     """out = hidden + y rounded to hidden's dtype (acceptmoe_residual_add)."""
@@ -386,7 +537,7 @@ def residual_norm(hidden: torch.Tensor, y: torch.Tensor | None, weight: torch.Te
             res["codes"] = torch.empty((T, H), dtype=torch.float8_e4m3fn, device=dev)
             res["scale"] = torch.empty((T, 1 if g < 0 else H // g), dtype=torch.float32, device=dev)
     else:
-        res = out
+        res = dict(out) if y is not None else {**out, "hidden": hidden}
         want = [("hidden", hidden.dtype, (T, H))] if y is not None else []
         want += ([("norm", hidden.dtype, (T, H))] if g == 0 else
                  [("codes", torch.float8_e4m3fn, (T, H)), ("scale", torch.float32, (T, 1 if g < 0 else H // g))])
@@ -505,27 +656,47 @@ class VerifyStack:
     one stream and allocates nothing, so a whole pass can be captured in one
     HIP graph.  The input of every layer stays in `h[l]` and each layer's
     logits, routing and output in its own buffers (for teacher-forced checks).
+
+    norms: len(layers) + 1 weight vectors [H] of the layer dtype.  With them every
+    layer takes the root-mean-square norm of its stream, kept in `x[l]`, and step()
+    returns the norm behind the last layer (what the output head reads); the
+    addition and the norm are one launch (residual_norm).
     """
 
-    def __init__(self, layers: list, max_tokens: int):
+    def __init__(self, layers: list, max_tokens: int, norms: list | None = None, eps: float = 1e-6):
         self.layers = layers
-        dev = layers[0].logits.device
-        self.h = [torch.empty((max_tokens, layers[0].H), dtype=layers[0].dtype, device=dev)
-                  for _ in range(len(layers) + 1)]
+        dev, dt, H = layers[0].logits.device, layers[0].dtype, layers[0].H
+        self.h = [torch.empty((max_tokens, H), dtype=dt, device=dev) for _ in range(len(layers) + 1)]
+        self.norms, self.eps = norms, eps
+        if norms is not None:
+            if len(norms) != len(layers) + 1:
+                raise ValueError(f"{len(layers)} layers need {len(layers) + 1} norms, got {len(norms)}")
+            for w in norms:
+                _need(w, "norm", dt, 1)
+                if w.shape[0] != H:
+                    raise ValueError(f"norms must have {H} elements")
+            self.x = [torch.empty((max_tokens, H), dtype=dt, device=dev) for _ in range(len(layers) + 1)]
 
     def twin(self) -> "VerifyStack":
         """Same weights, own buffers (a second block in flight)."""
-        return VerifyStack([ly.twin() for ly in self.layers], self.h[0].shape[0])
+        return VerifyStack([ly.twin() for ly in self.layers], self.h[0].shape[0], self.norms, self.eps)
 
     def step(self, h0, parent, depth, prob, tree_offsets=None, stream=None) -> torch.Tensor:
         T = h0.shape[0]
         if h0.data_ptr() != self.h[0].data_ptr():
             with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream()):
                 self.h[0][:T].copy_(h0)
+        if self.norms is None:
+            for l, layer in enumerate(self.layers):
+                _, _, y = layer.step(self.h[l][:T], parent, depth, prob, tree_offsets, stream=stream)
+                residual_add(self.h[l][:T], y, out=self.h[l + 1][:T], stream=stream)
+            return self.h[len(self.layers)][:T]
+        residual_norm(self.h[0][:T], None, self.norms[0], self.eps, out={"norm": self.x[0][:T]}, stream=stream)
         for l, layer in enumerate(self.layers):
-            _, _, y = layer.step(self.h[l][:T], parent, depth, prob, tree_offsets, stream=stream)
-            residual_add(self.h[l][:T], y, out=self.h[l + 1][:T], stream=stream)
-        return self.h[len(self.layers)][:T]
+            _, _, y = layer.step(self.x[l][:T], parent, depth, prob, tree_offsets, stream=stream)
+            residual_norm(self.h[l][:T], y, self.norms[l + 1], self.eps,
+                          out={"hidden": self.h[l + 1][:T], "norm": self.x[l + 1][:T]}, stream=stream)
+        return self.x[len(self.layers)][:T]
 
 
 # ---------------------------------------------------------------------------

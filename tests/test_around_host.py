@@ -85,3 +85,57 @@ def accept(token=A, parent=B, target=C, offs=None, trees=1, T=5, on=D, path=E, p
     ({"bonus": None}, L.ERR_INVALID_ARG, "null")])
 def test_accept_rejects(change, code, word):
     refused(accept(**change), code, word)
+
+
+# ---------------------------------------------------------------------------
+# experts in 4 bits
+# ---------------------------------------------------------------------------
+def fwd(hidden=A, wgu=B, wd=C, T=4, H=64, I=32, experts=8, k=2, idx=D, gate=D, out=E, ws=V(0x200000000), nbytes=1 << 40):
+    return L.lib().acceptmoe_moe_forward_q4(hidden, wgu, wd, T, H, I, experts, k, idx, gate, out, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("change,code,word", [
+    ({"T": -1}, L.ERR_INVALID_ARG, "T must"), ({"H": 48}, L.ERR_UNSUPPORTED, "multiples of 32"),
+    ({"I": 0}, L.ERR_UNSUPPORTED, "multiples of 32"), ({"H": 65568}, L.ERR_UNSUPPORTED, "65536"),
+    ({"experts": 513}, L.ERR_UNSUPPORTED, "E must"), ({"k": 0}, L.ERR_UNSUPPORTED, "k must"),
+    ({"k": 33}, L.ERR_UNSUPPORTED, "k must"), ({"T": 1 << 30}, L.ERR_UNSUPPORTED, "too large"),
+    ({"hidden": None}, L.ERR_INVALID_ARG, "null"), ({"wgu": None}, L.ERR_INVALID_ARG, "null"),
+    ({"wd": None}, L.ERR_INVALID_ARG, "null"), ({"idx": None}, L.ERR_INVALID_ARG, "null"),
+    ({"gate": None}, L.ERR_INVALID_ARG, "null"), ({"out": None}, L.ERR_INVALID_ARG, "null"),
+    ({"out": V(0x100008)}, L.ERR_INVALID_ARG, "aligned"), ({"ws": None}, L.ERR_WORKSPACE, "needs"),
+    ({"nbytes": 100}, L.ERR_WORKSPACE, "needs"), ({"ws": V(0x200000010)}, L.ERR_WORKSPACE, "aligned")])
+def test_forward_q4_rejects(change, code, word):
+    refused(fwd(**change), code, word)
+
+
+def test_q4_sizes():
+    lib = L.lib()
+    # a quad of 16-row tiles takes 4,352 bytes per 128 columns
+    assert lib.acceptmoe_q4_gate_up_bytes(8, 96, 256) == 8 * 3 * 2 * 4352
+    assert lib.acceptmoe_q4_down_bytes(8, 256, 96) == 8 * 4 * 1 * 4352
+    assert lib.acceptmoe_q4_down_bytes(8, 96, 160) == 8 * 2 * 2 * 4352
+    for bad in ((0, 96, 256), (8, 40, 256), (8, 96, 0), (513, 96, 256), (8, 65568, 32)):
+        assert lib.acceptmoe_q4_gate_up_bytes(*bad) == 0 and lib.acceptmoe_q4_down_bytes(*bad) == 0
+    sizes = [lib.acceptmoe_moe_forward_q4_workspace_size(t, 2048, 768, 128, 8) for t in range(300)]
+    assert sizes == sorted(sizes) and fwd(T=0) == L.OK
+    assert lib.acceptmoe_moe_forward_q4_workspace_size(-1, 2048, 768, 128, 8) == 0
+
+
+def test_q4_packing_rejects():
+    lib = L.lib()
+    refused(lib.acceptmoe_quantize_q4(A, 5, 64, B, C, None), L.ERR_INVALID_ARG, "dtype")
+    refused(lib.acceptmoe_quantize_q4(A, L.F32, 65, B, C, None), L.ERR_INVALID_ARG, "multiple of 32")
+    refused(lib.acceptmoe_quantize_q4(A, L.F32, 64, None, C, None), L.ERR_INVALID_ARG, "null")
+    refused(lib.acceptmoe_quantize_q4(A, L.F32, 64, V(0x100010), C, None), L.ERR_INVALID_ARG, "overlap")
+    refused(lib.acceptmoe_quantize_q4(V(0x100004), L.F32, 64, B, C, None), L.ERR_INVALID_ARG, "aligned")
+    assert lib.acceptmoe_quantize_q4(None, L.F32, 0, None, None, None) == L.OK
+    up = lib.acceptmoe_pack_gate_up_q4
+    refused(up(A, B, C, D, 4, 40, 64, E, None), L.ERR_UNSUPPORTED, "multiples of 32")
+    refused(up(A, B, C, None, 4, 32, 64, E, None), L.ERR_INVALID_ARG, "null")
+    refused(up(A, B, C, D, 4, 32, 64, A, None), L.ERR_INVALID_ARG, "overlaps")
+    refused(up(A, B, C, D, 4, 32, 64, V(0x100004), None), L.ERR_INVALID_ARG, "aligned")
+    down = lib.acceptmoe_pack_down_q4
+    refused(down(A, B, 0, 64, 32, E, None), L.ERR_UNSUPPORTED, "E must")
+    refused(down(None, B, 4, 64, 32, E, None), L.ERR_INVALID_ARG, "null")
+    refused(down(A, B, 4, 64, 32, B, None), L.ERR_INVALID_ARG, "overlaps")
+    refused(down(V(0x100008), B, 4, 64, 32, E, None), L.ERR_INVALID_ARG, "aligned")

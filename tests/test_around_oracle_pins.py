@@ -54,3 +54,33 @@ def test_accept_by_hand():
     on, paths, length, bonus = A.accept(token, parent, target, [0, 7, 7])
     assert paths == [[0, 1, 6], []] and length == [3, 0] and bonus == [42, -1]
     assert on.tolist() == [1, 1, 0, 0, 0, 0, 1]
+
+
+def test_q4_by_hand():
+    w = np.zeros(64)
+    w[:4] = 6.0, -0.25, 0.75, 5.0         # scale 1: 6, 0 (tie to even), 1, 4 (tie to even)
+    w[32:35] = 6.5, 1.0, -3.0             # above 6: scale 2
+    codes, scales = A.quantize_q4(w)
+    assert scales.tolist() == [127, 128]
+    v = A.dequantize_q4(codes, scales)
+    assert v[:4].tolist() == [6.0, 0.0, 1.0, 4.0] and np.signbit(v[1])
+    assert v[32:35].tolist() == [6.0, 1.0, -3.0]
+    assert codes[0] == 7 | (8 << 4) and codes[1] == 2 | (6 << 4)
+
+
+def test_q4_nearest():
+    rng = np.random.default_rng(0)
+    w = rng.standard_normal((50, 96)) * 2.0 ** rng.integers(-20, 20, (50, 1))
+    v = A.dequantize_q4(*A.quantize_q4(w))
+    scale = np.repeat(2.0 ** np.ceil(np.log2(np.abs(w).reshape(50, -1, 32).max(-1) / 6)), 32, axis=-1)
+    best = np.abs(w[..., None] - scale[..., None] * A.E2M1).min(-1)
+    assert np.array_equal(np.abs(w - v), best)
+
+
+def test_forward_equals_dense_formula():
+    rng = np.random.default_rng(1)
+    x, g, u, d = (rng.standard_normal(s) for s in ((3, 8), (4, 6, 8), (4, 6, 8), (4, 8, 6)))
+    idx, gate = [[0, 2], [3, 3], [-1, 9]], np.float64([[0.5, 0.25], [1.0, 7.0], [1.0, 1.0]])
+    ffn = lambda e, v: d[e] @ ((g[e] @ v) / (1 + np.exp(-(g[e] @ v))) * (u[e] @ v))  # noqa: E731
+    want = np.stack([0.5 * ffn(0, x[0]) + 0.25 * ffn(2, x[0]), ffn(3, x[1]), np.zeros(8)])
+    assert np.allclose(A.moe_forward(x, g, u, d, idx, gate), want, rtol=1e-13)
