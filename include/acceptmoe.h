@@ -383,15 +383,17 @@ int32_t acceptmoe_residual_norm(const void* hidden, int32_t dtype, const float* 
  * token -1 and prob 0.  Where logits are +inf, those tokens share the weight.
  *   logits       [R, V] device, `dtype` (F32 or BF16), row r at element
  *                r * row_stride (>= V), aligned to its element
- *   uniform      [R] device fp32, u in [0, 1) (values outside are clamped)
+ *   uniform      [R] device fp32, u in [0, 1) (values outside are clamped to
+ *                [0, 1 - 2^-24])
  *   temperature, top_p, min_p  [R] device fp32, or NULL: 1 / no filter
  *   top_k        [R] device int32, or NULL
  *   token, prob  [R] device int32 / fp32, written
  *   workspace    acceptmoe_sample_workspace_size(R, V) bytes, 256-byte aligned,
  *                not shared by calls that may run concurrently
  *   1 <= V <= ACCEPTMOE_MAX_VOCAB, R <= ACCEPTMOE_MAX_SAMPLE_ROWS; R == 0 is a no-op.
- * Exponentials are taken in 64 bits and summed as whole numbers of 2^-43, so the
- * result is deterministic and u falls between the borders that 64-bit sums give.
+ * Exponentials and sums are held in 64 bits, so u falls between the borders that
+ * 64-bit sums give (without top_k, weights below e^-31 of the largest may be left out
+ * of the sums); the result is deterministic.
  */
 size_t acceptmoe_sample_workspace_size(int32_t R, int32_t V);
 int32_t acceptmoe_sample(const void* logits, int32_t dtype, int64_t row_stride, int32_t R, int32_t V,

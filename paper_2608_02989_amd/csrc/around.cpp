@@ -118,6 +118,7 @@ int32_t acceptmoe_sample(const void* logits, int32_t dtype, int64_t row_stride, 
   p.min_p = min_p;
   p.token = token;
   p.prob = prob;
+  p.workspace = workspace;
   p.row_stride = static_cast<size_t>(row_stride);
   p.R = R;
   p.V = V;

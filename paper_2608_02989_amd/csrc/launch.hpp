@@ -137,6 +137,7 @@ struct SampleParams {
   int32_t* token;
   float* prob;
   size_t row_stride;  // elements
+  void* workspace;
   int R, V, is_bf16;
 };
 size_t sample_workspace_bytes(int R, int V);

@@ -65,8 +65,13 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* part) {
   return s;
 }
 
+// u as used: in [0, 1)
+__device__ __forceinline__ double row_uniform(const SampleParams& p, int r) {
+  return fmin(fmax(static_cast<double>(p.uniform[r]), 0.0), 1.0 - 1.0 / 16777216.0);
+}
+
 // ---------------------------------------------------------------------------
-// One workgroup per row, over the row in memory: a radix search by digits of 11,
+// Any row, by one workgroup over the row in memory: a radix search by digits of 11,
 // 11 and 10 bits of the key, with the weights (or counts) of each digit summed
 // in LDS.
 // ---------------------------------------------------------------------------
@@ -167,9 +172,8 @@ __device__ int find_index(const Row<kBf16>& row, uint32_t key, uint64_t r, RowSh
 }
 
 template <bool kBf16>
-__global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleParams p) {
-  __shared__ RowShared sh;
-  const int r = blockIdx.x, tid = threadIdx.x;
+__device__ void sample_row(const SampleParams& p, int r, RowShared& sh) {
+  const int tid = threadIdx.x;
   const Row<kBf16> row{static_cast<const char*>(p.logits) + r * p.row_stride * (kBf16 ? 2 : 4), p.V};
   uint32_t top = 0;
   for (int i = tid; i < p.V; i += kRowThreads) top = max(top, row.key(i));
@@ -227,8 +231,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleParams p)
     }
     total = block_sum(s, sh.part64);
   }
-  const double u = fmax(static_cast<double>(p.uniform[r]), 0.0);
-  const uint64_t need = min(static_cast<uint64_t>(u * static_cast<double>(total)) + 1, total);
+  const uint64_t need = min(static_cast<uint64_t>(row_uniform(p, r) * static_cast<double>(total)) + 1, total);
   const Place at = find_place<kBf16, false>(row, rule, need, sh);
   const uint64_t w = rule.fixed(at.key);
   const int i = find_index(row, at.key, (need - at.before + w - 1) / w, sh);
@@ -238,14 +241,704 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleParams p)
   }
 }
 
+
+// ---------------------------------------------------------------------------
+// The common cases in three launches that read a row once or twice, R x splits
+// workgroups wide.  What each does depends on the row's settings:
+//   greedy, or 0 < top_k <= kFastK: `scan` lists each split's candidates (the largest
+//     logits, at least top_k of them), `filter` (one workgroup of the row) cuts
+//     them to the top_k, sorts those and picks.
+//   no top_k: `scan` sums weights per bin of 1/32 in z / temperature, `filter` finds the
+//     bins in which the kept prefix ends and in which the sample lies, and lists
+//     the tokens of those, `finish` orders them and picks.
+//   other top_k, more candidates or tokens in a bin than the lists hold (many
+//     equal logits): `finish` runs sample_row.
+// ---------------------------------------------------------------------------
+constexpr int kScanThreads = 1024;
+constexpr int kFastK = 1000;        // one sorted candidate per thread
+constexpr int kCandCap = 1280;      // candidates of a split
+constexpr int kCandMax = 8192;      // candidates of a row (LDS)
+constexpr int kGridBins = 1024;     // 32 nats below the largest logit; weights beyond sum to less than 2^20 e^-31
+constexpr int kCopies = 4;          // of each bin, by lane, against LDS atomics on one address
+constexpr int kListCap = 4096;      // tokens of the listed bins
+constexpr int kRowsPerLaunch = 1024;
+constexpr int kMaxSplits = 64;
+constexpr double kPerNat = 32.0;
+
+enum class Mode { Greedy, TopK, Full, Slow };
+
+// a token as one number: larger logit, then lower index, is larger
+__device__ __forceinline__ unsigned long long token_order(uint32_t key, int index) {
+  return (static_cast<unsigned long long>(key) << 32) | (0xffffffffu - static_cast<uint32_t>(index));
+}
+__device__ __forceinline__ uint32_t order_key(unsigned long long v) { return static_cast<uint32_t>(v >> 32); }
+__device__ __forceinline__ int order_index(unsigned long long v) {
+  return static_cast<int>(0xffffffffu - static_cast<uint32_t>(v));
+}
+
+struct SplitPart {
+  uint32_t top;  // largest key of the split
+  int n;         // candidates (may exceed kCandCap: not all are here)
+  unsigned long long data[kCandCap];  // candidates, or the sums of kGridBins bins
+};
+static_assert(kGridBins <= kCandCap, "bins fit");
+
+struct RowPart {
+  int n_cut, n_pick;     // tokens listed (may exceed kListCap)
+  int t_cut;             // bin in which the kept prefix ends, -1: everything is kept
+  int t_pick0, t_pick1;  // bins in which the sample lies
+  int slow;              // finish with sample_row
+  uint32_t top;
+  double before_cut, before_pick, total, grid_top;
+  unsigned long long cut[kListCap], pick[kListCap];
+};
+
+__host__ __device__ inline size_t sample_part_bytes(int splits) {
+  return (sizeof(RowPart) + splits * sizeof(SplitPart) + 255) / 256 * 256;
+}
+
+struct RowView {
+  RowPart* row;
+  SplitPart* split;
+  __device__ RowView(const SampleParams& p, int local, int splits) {
+    char* base = static_cast<char*>(p.workspace) + local * sample_part_bytes(splits);
+    row = reinterpret_cast<RowPart*>(base);
+    split = reinterpret_cast<SplitPart*>(base + sizeof(RowPart));
+  }
+};
+
+__device__ __forceinline__ Mode row_mode(const SampleParams& p, int r) {
+  if (p.temperature && !(p.temperature[r] > 0.f)) return Mode::Greedy;
+  const int k = p.top_k ? p.top_k[r] : 0;
+  if (k <= 0 || k >= p.V) return Mode::Full;
+  return k <= kFastK ? Mode::TopK : Mode::Slow;
+}
+
+// z / temperature in bins of 1/32: the whole part names the bin, the rest gives the
+// weight within it, exp(rest / 32) in [1, 1.032).  A bin's sum of these does not depend
+// on the row's largest logit, so splits are added without knowing it.
+struct Grid {
+  double scale;
+  __device__ __forceinline__ double at(uint32_t key) const { return key_logit(key) * scale; }
+  static __device__ __forceinline__ double weight(double rest) {
+    // y = rest / 32 < 2^-5: the series up to y^6 / 720 is off by less than 6e-15
+    const double y = rest * (1.0 / kPerNat);
+    double v = fma(y, 1.0 / 720, 1.0 / 120);
+    v = fma(y, v, 1.0 / 24);
+    v = fma(y, v, 1.0 / 6);
+    v = fma(y, v, 0.5);
+    v = fma(y, v, 1.0);
+    return fma(y, v, 1.0);
+  }
+};
+
+// the pieces of 16 bytes that hold a split of a row, in registers; places outside the row are -inf
+template <bool kBf16, int NV>
+struct Pieces {
+  static constexpr int kPer = kBf16 ? 8 : 4;  // tokens of a piece
+  uint4 v[NV];
+  int first;  // token index of this thread's first piece's first place
+
+  __device__ __forceinline__ void load(const SampleParams& p, int r, int s) {
+    const char* row = static_cast<const char*>(p.logits) + r * p.row_stride * (kBf16 ? 2 : 4);
+    const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(row) % 16) / (kBf16 ? 2 : 4);
+    const uint4* base = reinterpret_cast<const uint4*>(row - skew * (kBf16 ? 2 : 4));
+    const int q0 = s * kScanThreads * NV + static_cast<int>(threadIdx.x);
+    first = q0 * kPer - skew;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int e0 = first + i * kScanThreads * kPer;
+      v[i] = kBf16 ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u)
+                   : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
+      if (e0 >= 0 && e0 + kPer <= p.V) {
+        v[i] = base[q0 + i * kScanThreads];
+      } else if (e0 + kPer > 0 && e0 < p.V) {  // the row's first or last piece
+        uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+          if (e0 + j < 0 || e0 + j >= p.V) continue;
+          if (kBf16) {
+            const uint32_t h = reinterpret_cast<const uint16_t*>(row)[e0 + j];
+            w[j / 2] = j % 2 ? (w[j / 2] & 0xffffu) | (h << 16) : (w[j / 2] & 0xffff0000u) | h;
+          } else {
+            w[j] = reinterpret_cast<const uint32_t*>(row)[e0 + j];
+          }
+        }
+        v[i] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+  __device__ __forceinline__ float logit(int i, int j) const {
+    const uint32_t w = (kBf16 ? j / 2 : j) == 0 ? v[i].x : (kBf16 ? j / 2 : j) == 1 ? v[i].y : (kBf16 ? j / 2 : j) == 2 ? v[i].z : v[i].w;
+    return __uint_as_float(kBf16 ? (j % 2 ? w & 0xffff0000u : w << 16) : w);
+  }
+  __device__ __forceinline__ int index(int i, int j) const { return first + i * kScanThreads * kPer + j; }
+  // largest logit of a piece; NaN never wins
+  __device__ __forceinline__ float largest(int i) const {
+    float m = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) m = fmaxf(m, logit(i, j));
+    return m;
+  }
+};
+
+// Workgroup-wide number of the values a thread counts by ballot; one barrier a call,
+// calls in a row alternate between two halves of `part`.
+__device__ __forceinline__ int block_count(int wave_count, int* part, int turn) {
+  constexpr int kWaves = kScanThreads / kWave;
+  int* half = part + (turn & 1) * kWaves;
+  if (lane_id() == 0) half[wave_id()] = wave_count;
+  __syncthreads();
+  const int v = half[lane_id() % kWaves];
+  return wave_sum_i32(v) / (kWave / kWaves);
+}
+
+// The largest cut, at least `lo`, with count(cut) >= need, or one before it whose count is
+// at most `enough`; count() falls from count(lo) >= need on and is 0 above hi.
+template <class T, class Count>
+__device__ __forceinline__ T bisect(T lo, T hi, int need, int enough, Count count) {
+  while (lo < hi) {
+    const T mid = hi - (hi - lo) / 2;
+    const int c = count(mid);
+    if (c >= need) {
+      lo = mid;
+      if (c <= enough) break;
+    } else {
+      hi = mid - 1;
+    }
+  }
+  return lo;
+}
+
+template <bool kBf16, int NV>
+__global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(8))) void sample_scan_kernel(
+    SampleParams p, int row0, int splits) {
+  __shared__ unsigned long long s_bin[kGridBins * kCopies];
+  __shared__ uint32_t s_max[kScanThreads / kWave];
+  __shared__ int s_part[2 * kScanThreads / kWave];
+  __shared__ int s_n;
+  const int local = blockIdx.x / splits, r = row0 + local, s = blockIdx.x % splits, tid = threadIdx.x;
+  const Mode mode = row_mode(p, r);
+  const RowView ws(p, local, splits);
+  SplitPart& out = ws.split[s];
+  if (s == 0 && tid == 0) {
+    ws.row->n_cut = ws.row->n_pick = 0;
+    ws.row->slow = mode == Mode::Slow;
+  }
+  if (mode == Mode::Slow) return;
+  Pieces<kBf16, NV> z;
+  z.load(p, r, s);
+  if (tid == 0) s_n = 0;
+  if (mode == Mode::Full)
+    for (int i = tid; i < kGridBins * kCopies; i += kScanThreads) s_bin[i] = 0;
+  uint32_t most[NV], top = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    most[i] = token_key(z.largest(i));
+    top = max(top, most[i]);
+  }
+  top = block_max(top, s_max);  // orders the clearing above, too
+  if (tid == 0) out.top = top;
+  if (top <= kKeyNegInf) {
+    if (tid == 0) out.n = 0;
+    return;
+  }
+  if (mode == Mode::Full) {
+    const Grid grid{kPerNat / (p.temperature ? static_cast<double>(p.temperature[r]) : 1.0)};
+    const double grid_top = floor(grid.at(top));
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+      for (int j = 0; j < Pieces<kBf16, NV>::kPer; ++j) {
+        const double g = static_cast<double>(z.logit(i, j)) * grid.scale, b = floor(g);
+        const double t = grid_top - b;
+        if (t >= 0.0 && t < kGridBins) {
+          // weight 2^43 rounded to a whole number in the low bits of the sum
+          const double w = fma(Grid::weight(g - b), kWeightOne, 4503599627370496.0);
+          atomicAdd(&s_bin[static_cast<int>(t) * kCopies + (tid & (kCopies - 1))],
+                    static_cast<unsigned long long>(__double_as_longlong(w)) & 0xfffffffffffffull);
+        }
+      }
+    }
+    __syncthreads();
+    unsigned long long sum = 0;
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) sum += s_bin[tid * kCopies + c];
+    out.data[tid] = sum;
+    return;
+  }
+  uint32_t cut = top;
+  if (mode == Mode::TopK) {
+    // At least k pieces reach the k-th largest of the pieces' largest logits, so at
+    // least k tokens do, and few more while there are many more pieces than k.
+    const int k = p.top_k[r];
+    int turn = 0;
+    auto pieces = [&](uint32_t least) {
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) c += popc64(__ballot(most[i] >= least));
+      return block_count(c, s_part, turn++);
+    };
+    cut = kKeyNegInf + 1;
+    if (pieces(cut) >= k) cut = bisect<uint32_t>(cut, top, k, k + k / 8 + 8, pieces);
+    auto tokens = [&](uint32_t least) {
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        if (__ballot(most[i] >= least) == 0) continue;
+#pragma unroll
+        for (int j = 0; j < Pieces<kBf16, NV>::kPer; ++j) c += popc64(__ballot(token_key(z.logit(i, j)) >= least));
+      }
+      return block_count(c, s_part, turn++);
+    };
+    // many tokens per piece reach it only when k is a good part of the pieces
+    if (k > kCandCap / 4 && tokens(cut) > kCandCap) cut = bisect<uint32_t>(cut, top, k, kCandCap, tokens);
+  }
+  if (mode == Mode::Greedy) {
+    // the lowest index of the largest logit
+    uint32_t best = 0;
+#pragma unroll
+    for (int i = NV - 1; i >= 0; --i) {
+      if (most[i] != top) continue;
+#pragma unroll
+      for (int j = Pieces<kBf16, NV>::kPer - 1; j >= 0; --j)
+        if (token_key(z.logit(i, j)) == top) best = 0xffffffffu - static_cast<uint32_t>(z.index(i, j));
+    }
+    best = block_max(best, s_max);
+    if (tid == 0) {
+      out.n = 1;
+      out.data[0] = (static_cast<unsigned long long>(top) << 32) | best;
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    if (most[i] < cut) continue;
+#pragma unroll
+    for (int j = 0; j < Pieces<kBf16, NV>::kPer; ++j) {
+      const uint32_t key = token_key(z.logit(i, j));
+      if (key >= cut) {
+        const int at = atomicAdd(&s_n, 1);
+        if (at < kCandCap) out.data[at] = token_order(key, z.index(i, j));
+      }
+    }
+  }
+  __syncthreads();
+  if (tid == 0) out.n = s_n;
+}
+
+// one value per thread, descending over the first n threads (n a power of two from 64 on);
+// the other threads' values must be no larger
+__device__ __forceinline__ unsigned long long block_sort(unsigned long long v, int n, unsigned long long* buf) {
+  const int tid = threadIdx.x;
+  for (int run = 2; run <= n; run *= 2) {
+    for (int j = run / 2; j > 0; j /= 2) {
+      unsigned long long o;
+      if (j >= kWave) {
+        __syncthreads();
+        buf[tid] = v;
+        __syncthreads();
+        o = buf[tid ^ j];
+      } else {
+        o = __shfl_xor(v, j);
+      }
+      const bool larger = ((tid & run) == 0) == ((tid & j) == 0);
+      v = larger == (v > o) ? v : o;
+    }
+  }
+  return v;
+}
+
+// inclusive running sum over the workgroup, in thread order
+__device__ __forceinline__ double block_scan(double v, double* part) {
+  for (int o = 1; o < kWave; o <<= 1) {
+    const double u = __shfl_up(v, o);
+    if (lane_id() >= o) v += u;
+  }
+  __syncthreads();
+  if (lane_id() == kWave - 1) part[wave_id()] = v;
+  __syncthreads();
+  double before = 0.0;
+  for (int w = 0; w < wave_id(); ++w) before += part[w];
+  return before + v;
+}
+
+// Orders n listed tokens, one per thread, and gives each its weight and running sum.
+struct Sorted {
+  unsigned long long token;
+  double weight, sum;  // sum includes the token's own
+};
+template <class Weight>
+__device__ __forceinline__ Sorted sort_and_sum(unsigned long long v, int n, unsigned long long* buf, double* part,
+                                               Weight weight) {
+  int size = kWave;
+  while (size < n) size *= 2;
+  const unsigned long long token = block_sort(v, size, buf);
+  const double w = static_cast<int>(threadIdx.x) < n ? weight(order_key(token)) : 0.0;
+  return {token, w, block_scan(w, part)};
+}
+
+struct PickShared {
+  unsigned long long cand[kCandMax];
+  unsigned long long buf[kScanThreads];
+  double part[kScanThreads / kWave];
+  double value;
+  int part32[2 * kScanThreads / kWave];
+  int n, at;
+};
+
+// smallest thread index where `hit` (monotone or not) holds, n if none
+__device__ __forceinline__ int first_thread(bool hit, int n, PickShared& sh) {
+  __syncthreads();
+  if (threadIdx.x == 0) sh.at = n;
+  __syncthreads();
+  const uint64_t m = __ballot(hit);
+  if (m != 0 && lane_id() == 0) atomicMin(&sh.at, wave_id() * kWave + __builtin_ctzll(m));
+  __syncthreads();
+  return sh.at;
+}
+
+// the value of thread `at`
+__device__ __forceinline__ double thread_value(double v, int at, PickShared& sh) {
+  __syncthreads();
+  if (static_cast<int>(threadIdx.x) == at) sh.value = v;
+  __syncthreads();
+  return sh.value;
+}
+
+// Candidates of a greedy or top-k row -> token.  False: the lists do not hold them all.
+__device__ bool pick_candidates(const SampleParams& p, int r, Mode mode, const RowView& ws, int splits, PickShared& sh) {
+  const int tid = threadIdx.x;
+  uint32_t top = 0;
+  int n = 0;
+  bool whole = true;
+  for (int s = 0; s < splits; ++s) {
+    const int ns = ws.split[s].n;
+    whole = whole && ns <= kCandCap && n + ns <= kCandMax;
+    if (!whole) return false;
+    top = max(top, ns > 0 ? ws.split[s].top : 0u);
+    for (int i = tid; i < ns; i += kScanThreads) sh.cand[n + i] = ws.split[s].data[i];
+    n += ns;
+  }
+  if (n == 0) {
+    if (tid == 0) p.token[r] = -1, p.prob[r] = 0.f;
+    return true;
+  }
+  __syncthreads();
+  if (mode == Mode::Greedy) {
+    if (tid < kWave) {
+      unsigned long long best = tid < n ? sh.cand[tid] : 0;  // one a split, kMaxSplits at most
+      for (int o = 32; o >= 1; o >>= 1) best = max(best, __shfl_xor(best, o));
+      if (tid == 0) p.token[r] = order_index(best), p.prob[r] = 1.f;
+    }
+    return true;
+  }
+  const int k = min(p.top_k[r], n);
+  unsigned long long v = tid < n ? sh.cand[tid] : 0;
+  if (n > k || n > kScanThreads) {
+    constexpr int kMine = kCandMax / kScanThreads;
+    unsigned long long mine[kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) mine[i] = tid + i * kScanThreads < n ? sh.cand[tid + i * kScanThreads] : 0;
+    int turn = 0;
+    const unsigned long long cut =
+        bisect<unsigned long long>(1, token_order(top, 0), k, k, [&](unsigned long long least) {
+          int c = 0;
+#pragma unroll
+          for (int i = 0; i < kMine; ++i)
+            if (i * kScanThreads < n) c += popc64(__ballot(mine[i] >= least));
+          return block_count(c, sh.part32, turn++);
+        });
+    __syncthreads();
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kMine; ++i)
+      if (mine[i] >= cut) sh.buf[atomicAdd(&sh.n, 1)] = mine[i];  // exactly k
+    __syncthreads();
+    v = tid < k ? sh.buf[tid] : 0;
+  }
+  const float tau = p.temperature ? p.temperature[r] : 1.f;
+  const RowRule rule{top, key_logit(top), tau};
+  const Sorted t = sort_and_sum(v, k, sh.buf, sh.part, [&](uint32_t key) { return rule.weight(key); });
+  int keep = k;
+  if (p.top_p && !(p.top_p[r] >= 1.f)) {
+    const double want = fmax(static_cast<double>(p.top_p[r]), 0.0) * thread_value(t.sum, k - 1, sh);
+    keep = min(keep, first_thread(tid < k && t.sum >= want, k, sh) + 1);
+  }
+  if (p.min_p && p.min_p[r] > 0.f)
+    keep = min(keep, first_thread(tid >= k || t.weight < fmin(static_cast<double>(p.min_p[r]), 1.0), k, sh));
+  keep = max(keep, 1);
+  const double total = thread_value(t.sum, keep - 1, sh);
+  const double at = row_uniform(p, r) * total;
+  if (tid == first_thread(tid < keep && t.sum > at, keep - 1, sh)) {
+    p.token[r] = order_index(t.token);
+    p.prob[r] = static_cast<float>(t.weight / total);
+  }
+  return true;
+}
+
+template <bool kBf16, int NV>
+__global__ __launch_bounds__(kScanThreads) void sample_filter_kernel(SampleParams p, int row0, int splits) {
+  __shared__ PickShared sh;
+  __shared__ int s_cut, s_first, s_last;
+  const int local = blockIdx.x / splits, r = row0 + local, s = blockIdx.x % splits, tid = threadIdx.x;
+  const Mode mode = row_mode(p, r);
+  const RowView ws(p, local, splits);
+  if (mode == Mode::Slow) return;
+  if (mode != Mode::Full) {
+    if (s == 0 && !pick_candidates(p, r, mode, ws, splits, sh) && tid == 0) ws.row->slow = 1;
+    return;
+  }
+  uint32_t top = 0;
+  for (int i = 0; i < splits; ++i) top = max(top, ws.split[i].top);
+  const double tau = p.temperature ? static_cast<double>(p.temperature[r]) : 1.0;
+  const Grid grid{kPerNat / tau};
+  const double grid_top = floor(grid.at(top));
+  // far from 0 the grid's 64 bits no longer hold the weights' digits
+  const bool slow = !(fabs(grid.at(top)) < 33554432.0);
+  if (s == 0 && tid == 0) {
+    ws.row->top = top;
+    ws.row->slow = slow && top > kKeyNegInf;
+    ws.row->grid_top = grid_top;
+  }
+  if (top <= kKeyNegInf || slow) return;
+  // thread t: the row's sum in bin t below its largest logit
+  unsigned long long sum = 0;
+  for (int i = 0; i < splits; ++i) {
+    const uint32_t part_top = ws.split[i].top;
+    if (part_top <= kKeyNegInf) continue;
+    const double at = tid - (grid_top - floor(grid.at(part_top)));
+    if (at >= 0.0) sum += ws.split[i].data[static_cast<int>(at)];
+  }
+  const double w = static_cast<double>(sum) / kWeightOne * exp(-tid / kPerNat);
+  const double incl = block_scan(w, sh.part), excl = incl - w;
+  const double total = thread_value(incl, kScanThreads - 1, sh);
+  int cut = -1;
+  double kept = total, least = total;  // the kept sum lies between
+  if (p.top_p && !(p.top_p[r] >= 1.f)) {
+    const double want = fmax(static_cast<double>(p.top_p[r]), 0.0) * total;
+    cut = min(first_thread(incl >= want, kScanThreads - 1, sh), kScanThreads - 1);
+  }
+  if (p.min_p && p.min_p[r] > 0.f) {
+    const double m = fmin(static_cast<double>(p.min_p[r]), 1.0);
+    const double t = grid_top - floor(grid.at(top) + kPerNat * log(m));
+    if (t < (cut < 0 ? kScanThreads : cut)) cut = static_cast<int>(t);
+  }
+  if (cut >= 0) {
+    kept = thread_value(incl, cut, sh);
+    least = thread_value(excl, cut, sh);
+  }
+  const double u = row_uniform(p, r);
+  // the last bin that holds a kept weight, for roundings at the end
+  const int last = cut >= 0 ? cut : first_thread(incl >= total, kScanThreads - 1, sh);
+  const int pick0 = min(first_thread(incl > u * least, last, sh), last);
+  const int pick1 = min(first_thread(incl > u * kept, last, sh), last);
+  if (s == 0) {
+    if (tid == pick0) ws.row->before_pick = excl;
+    if (tid == cut) ws.row->before_cut = excl;
+    if (tid == 0) {
+      ws.row->t_cut = cut;
+      ws.row->t_pick0 = pick0;
+      ws.row->t_pick1 = pick1;
+      ws.row->total = total;
+    }
+  }
+  Pieces<kBf16, NV> z;
+  z.load(p, r, s);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+#pragma unroll
+    for (int j = 0; j < Pieces<kBf16, NV>::kPer; ++j) {
+      const float logit = z.logit(i, j);
+      const double t = grid_top - floor(static_cast<double>(logit) * grid.scale);
+      if (t == cut) {
+        const int at = atomicAdd(&ws.row->n_cut, 1);
+        if (at < kListCap) ws.row->cut[at] = token_order(token_key(logit), z.index(i, j));
+      }
+      if (t >= pick0 && t <= pick1) {
+        const int at = atomicAdd(&ws.row->n_pick, 1);
+        if (at < kListCap) ws.row->pick[at] = token_order(token_key(logit), z.index(i, j));
+      }
+    }
+  }
+}
+
+union FinishShared {
+  RowShared row;
+  PickShared pick;
+};
+
+// The tokens around one place of a listed range of bins, one per thread.
+struct Near {
+  unsigned long long token;  // of this thread; 0 from n on
+  int n;
+  double before;  // weights of the row in front of them
+};
+
+// From a list of n <= kListCap tokens in `bins` bins from bin t0 on, those around the place
+// where passes(running sum) turns true, or of finer bin `limit` if that comes first.
+// A short list is taken as it is; a longer one is cut into kScanThreads finer bins, whose sums
+// are whole numbers, too.  n > kScanThreads: too many (equal logits).
+template <class Passes>
+__device__ __forceinline__ Near tokens_near(const unsigned long long* list, int n, const Grid& grid, double grid_top,
+                                            int t0, int bins, double before, int limit, PickShared& sh, Passes passes) {
+  const int tid = threadIdx.x;
+  if (n <= kScanThreads) return {tid < n ? list[tid] : 0, n, before};
+  constexpr int kMine = kListCap / kScanThreads;
+  unsigned long long* fine = sh.cand;
+  __syncthreads();
+  fine[tid] = 0;
+  if (tid == 0) sh.n = 0;
+  __syncthreads();
+  int sub[kMine];
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    sub[i] = -1;
+    if (tid + i * kScanThreads >= n) continue;
+    const double g = grid.at(order_key(list[tid + i * kScanThreads])), b = floor(g);
+    // the bin's own tokens run from its top (rest near 1) down
+    const double place = (grid_top - b - t0 + (1.0 - (g - b))) * (kScanThreads / static_cast<double>(bins));
+    sub[i] = min(max(static_cast<int>(place), 0), kScanThreads - 1);
+    const double w = Grid::weight(g - b) * exp((b + t0 - grid_top) / kPerNat);
+    atomicAdd(&fine[sub[i]], static_cast<unsigned long long>(__double2ull_rn(w * kWeightOne)));
+  }
+  __syncthreads();
+  const double w = static_cast<double>(fine[tid]) / kWeightOne * exp(-t0 / kPerNat);
+  const double incl = before + block_scan(w, sh.part);
+  const int at = min(first_thread(passes(incl), kScanThreads - 1, sh), limit);
+  const double front = thread_value(incl - w, at, sh);
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    if (sub[i] != at) continue;
+    const int k = atomicAdd(&sh.n, 1);
+    if (k < kScanThreads) sh.buf[k] = list[tid + i * kScanThreads];
+  }
+  __syncthreads();
+  return {tid < sh.n ? sh.buf[tid] : 0, sh.n, front};
+}
+
+template <bool kBf16>
+__global__ __launch_bounds__(kRowThreads) void sample_finish_kernel(SampleParams p, int row0, int splits) {
+  __shared__ FinishShared un;
+  const int local = blockIdx.x, r = row0 + local, tid = threadIdx.x;
+  const RowView ws(p, local, splits);
+  const RowPart& in = *ws.row;
+  if (in.slow) {
+    sample_row<kBf16>(p, r, un.row);
+    return;
+  }
+  if (row_mode(p, r) != Mode::Full) return;
+  const uint32_t top = in.top;
+  if (top <= kKeyNegInf) {
+    if (tid == 0) p.token[r] = -1, p.prob[r] = 0.f;
+    return;
+  }
+  const int n_cut = in.t_cut >= 0 ? in.n_cut : 0, n_pick = in.n_pick;
+  bool fits = n_cut <= kListCap && n_pick <= kListCap;
+  PickShared& sh = un.pick;
+  const double tau = p.temperature ? static_cast<double>(p.temperature[r]) : 1.0;
+  const Grid grid{kPerNat / tau};
+  const double grid_top = in.grid_top;
+  auto weight = [&](uint32_t key) {
+    const double g = grid.at(key), b = floor(g);
+    return Grid::weight(g - b) * exp((b - grid_top) / kPerNat);
+  };
+  double total = in.total;
+  if (fits && in.t_cut >= 0) {
+    const bool by_p = p.top_p && !(p.top_p[r] >= 1.f), by_m = p.min_p && p.min_p[r] > 0.f;
+    const double want = by_p ? fmax(static_cast<double>(p.top_p[r]), 0.0) * total : INFINITY;
+    const double m = by_m ? fmin(static_cast<double>(p.min_p[r]), 1.0) : 0.0;
+    int limit = kScanThreads - 1;
+    if (by_m) {  // the finer bin of the smallest weight that min_p keeps
+      const double place = grid_top + 1.0 - in.t_cut - (grid.at(top) + kPerNat * log(m));
+      limit = static_cast<int>(fmin(fmax(place * kScanThreads, 0.0), static_cast<double>(limit)));
+    }
+    const Near near = tokens_near(in.cut, n_cut, grid, grid_top, in.t_cut, 1, in.before_cut, limit, sh,
+                                  [&](double sum) { return sum >= want; });
+    fits = near.n <= kScanThreads;
+    if (fits) {
+      const RowRule rule{top, key_logit(top), tau};
+      const Sorted t = sort_and_sum(near.token, near.n, sh.buf, sh.part, weight);
+      int keep = near.n;
+      if (by_p) keep = min(keep, first_thread(tid < keep && near.before + t.sum >= want, near.n, sh) + 1);
+      if (by_m)
+        keep = min(keep, first_thread(tid >= near.n || rule.weight(order_key(t.token)) < m, near.n, sh));
+      total = near.before + (keep > 0 ? thread_value(t.sum, keep - 1, sh) : 0.0);
+    }
+  }
+  if (fits) {
+    const double at = row_uniform(p, r) * total;
+    const Near near = tokens_near(in.pick, n_pick, grid, grid_top, in.t_pick0, in.t_pick1 - in.t_pick0 + 1,
+                                  in.before_pick, kScanThreads - 1, sh, [&](double sum) { return sum > at; });
+    fits = near.n <= kScanThreads;
+    if (fits) {
+      const Sorted t = sort_and_sum(near.token, near.n, sh.buf, sh.part, weight);
+      if (tid == first_thread(tid < near.n && near.before + t.sum > at, near.n - 1, sh)) {
+        p.token[r] = order_index(t.token);
+        p.prob[r] = static_cast<float>(t.weight / total);
+      }
+    }
+  }
+  if (!fits) {
+    __syncthreads();
+    sample_row<kBf16>(p, r, un.row);
+  }
+}
+
+// 16-byte pieces per thread: 32 tokens' worth, or fewer while that spreads a row over more
+// workgroups of an otherwise idle device
+struct Shape {
+  int nv, splits;
+};
+Shape sample_shape(int R, int V, int is_bf16) {
+  const int per = is_bf16 ? 8 : 4;
+  const int pieces = (V + 2 * per - 2) / per;  // wherever the row starts
+  auto splits = [&](int nv) { return (pieces + kScanThreads * nv - 1) / (kScanThreads * nv); };
+  int nv = 32 / per;
+  while (nv > 1 && splits(nv / 2) > splits(nv) && splits(nv / 2) <= 16 && R * splits(nv / 2) <= 512) nv /= 2;
+  return {nv, splits(nv)};
+}
+
+template <bool kBf16, int NV>
+hipError_t launch_sample_nv(const SampleParams& p, int splits, hipStream_t stream) {
+  for (int row0 = 0; row0 < p.R; row0 += kRowsPerLaunch) {
+    const int rows = p.R - row0 < kRowsPerLaunch ? p.R - row0 : kRowsPerLaunch;
+    sample_scan_kernel<kBf16, NV><<<rows * splits, kScanThreads, 0, stream>>>(p, row0, splits);
+    sample_filter_kernel<kBf16, NV><<<rows * splits, kScanThreads, 0, stream>>>(p, row0, splits);
+    sample_finish_kernel<kBf16><<<rows, kRowThreads, 0, stream>>>(p, row0, splits);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <bool kBf16>
+hipError_t launch_sample_type(const SampleParams& p, hipStream_t stream) {
+  const Shape sh = sample_shape(p.R, p.V, kBf16);
+  switch (sh.nv) {
+    case 1: return launch_sample_nv<kBf16, 1>(p, sh.splits, stream);
+    case 2: return launch_sample_nv<kBf16, 2>(p, sh.splits, stream);
+    case 4: return launch_sample_nv<kBf16, 4>(p, sh.splits, stream);
+    default: break;
+  }
+  if constexpr (kBf16) return hipErrorInvalidValue;  // 32 tokens are four pieces
+  else return launch_sample_nv<false, 8>(p, sh.splits, stream);
+}
+
 }  // namespace
 
-size_t sample_workspace_bytes(int, int) { return 256; }
+// One size for both types: an fp32 row has more splits.  Grows with R: rows are spread
+// over at most min(512, 16 R) workgroups or take the splits of 32 tokens per thread.
+size_t sample_workspace_bytes(int R, int V) {
+  const size_t rows = R < kRowsPerLaunch ? R : kRowsPerLaunch;
+  const size_t whole = rows * ((V + 6) / 4 / (kScanThreads * 8) + 1);
+  const size_t spread = rows < 32 ? 16 * rows : 512;
+  return rows * (sizeof(RowPart) + 256) + (whole > spread ? whole : spread) * sizeof(SplitPart);
+}
 
 hipError_t launch_sample(const SampleParams& p, hipStream_t stream) {
-  if (p.is_bf16) sample_row_kernel<true><<<p.R, kRowThreads, 0, stream>>>(p);
-  else sample_row_kernel<false><<<p.R, kRowThreads, 0, stream>>>(p);
-  return hipGetLastError();
+  return p.is_bf16 ? launch_sample_type<true>(p, stream) : launch_sample_type<false>(p, stream);
 }
 
 }  // namespace amoe

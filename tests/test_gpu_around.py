@@ -107,8 +107,8 @@ def test_residual_norm_zero_rows_and_in_place(gpu):
 # sampling
 # ---------------------------------------------------------------------------
 def check_sample(z, u, dtype=torch.float32, stride=None, **rules):
-    """Tokens equal to the oracle's; u and top_p's sum at least 1e-9 of the sum of weights off
-    any border (the kernel's sums are off by at most V 2^-44 of the largest weight)."""
+    """Tokens equal to the oracle's, u and top_p's sum being further off any border than 64-bit
+    sums may move it (the oracle's margin)."""
     z = torch.as_tensor(z).to(dtype)
     R, V = z.shape
     zd = z.to(DEV)
@@ -131,7 +131,7 @@ def check_sample(z, u, dtype=torch.float32, stride=None, **rules):
     assert untouched(raw_t) and untouched(raw_p)
     for r in range(R):
         t, p, margin = A.sample_row(z[r].double().numpy(), u[r], **{n: a[r] for n, a in host.items()})
-        assert margin > 1e-9, (r, margin)
+        assert margin > 1, (r, margin)
         assert outs[0][0][r] == t, (r, outs[0][0][r], t, margin)
         # V 2^-44 of the sum and 64-bit work, then one rounding
         assert abs(outs[0][1][r] - p) <= p * (2.0 ** -24 + 1e-7), (r, outs[0][1][r], p)
@@ -190,6 +190,40 @@ def test_sample_hard_rows(gpu, V):
                                {"top_k": 64, "top_p": 0.93, "min_p": 0.01, "temperature": 5.0})):
         say("hard rows", V, rules)
         check_sample(z, 0.0437 + 0.9 * np.random.default_rng(100 + i).random(R), **rules)
+
+
+@pytest.mark.parametrize("spread", [0.02, 0.3, 1.0])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_sample_crowded(gpu, spread, dtype):
+    """Many tokens of nearly one weight: thousands within 1/32 of a nat, in bf16 mostly equal."""
+    rng = np.random.default_rng(int(spread * 100))
+    R, V = 4, 150001
+    z = (rng.standard_normal((R, V)) * spread).astype(np.float32)
+    for rules in ({}, {"top_p": 0.6}, {"min_p": 0.3}, {"top_p": 0.9, "min_p": 0.5}, {"top_k": 900}, {"top_k": 1000},
+                  {"top_k": 1001}, {"top_k": 64, "temperature": 40.0}, {"temperature": 1e4}):
+        say("crowded", spread, dtype, rules)
+        check_sample(z, rng.random(R), dtype, **rules)
+
+
+@pytest.mark.parametrize("R,V,dtype", [(33, 1023, torch.bfloat16), (257, 4097, torch.float32), (1100, 515, torch.float32),
+                                       (2, 262147, torch.bfloat16), (1, 1 << 20, torch.float32)])
+def test_sample_shapes(gpu, R, V, dtype):
+    """Rows spread over one to many workgroups, more rows than one launch takes, every row start's alignment."""
+    rng = np.random.default_rng(V)
+    z = logits(rng, R, V)
+    for rules in ({"top_k": 20, "top_p": 0.9}, {"top_p": 0.95}, {"temperature": 0.0}):
+        say("shape", R, V, rules)
+        check_sample(z, rng.random(R), dtype, **rules)
+
+
+def test_sample_far_from_zero(gpu):
+    """Logits with a large common part, of which the weights keep nothing."""
+    rng = np.random.default_rng(9)
+    z = np.round(rng.standard_normal((6, 9001)) * 3 * 64) / 64
+    z += np.float64([1e3, -1e3, 3e4, 1e5, -1e5, 0])[:, None]
+    for rules in ({}, {"top_p": 0.9, "min_p": 0.01}, {"top_k": 100}, {"temperature": 0.1}):
+        say("far", rules)
+        check_sample(z.astype(np.float32), rng.random(6), **rules)
 
 
 def test_sample_borders_of_u_and_top_p(gpu):
