@@ -70,6 +70,25 @@ __device__ __forceinline__ double row_uniform(const SampleParams& p, int r) {
   return fmin(fmax(static_cast<double>(p.uniform[r]), 0.0), 1.0 - 1.0 / 16777216.0);
 }
 
+// the workgroup's largest `high` and smallest `low`
+__device__ __forceinline__ void block_range(uint32_t& high, uint32_t& low, uint32_t* part) {
+  const int waves = static_cast<int>(blockDim.x) / kWave;
+  for (int o = 32; o >= 1; o >>= 1) {
+    high = max(high, static_cast<uint32_t>(__shfl_xor(high, o)));
+    low = min(low, static_cast<uint32_t>(__shfl_xor(low, o)));
+  }
+  __syncthreads();
+  if (lane_id() == 0) {
+    part[wave_id()] = high;
+    part[waves + wave_id()] = low;
+  }
+  __syncthreads();
+  for (int w = 0; w < waves; ++w) {
+    high = max(high, part[w]);
+    low = min(low, part[waves + w]);
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Any row, by one workgroup over the row in memory: a radix search by digits of 11,
 // 11 and 10 bits of the key, with the weights (or counts) of each digit summed
@@ -261,7 +280,6 @@ constexpr int kCandMax = 8192;      // candidates of a row (registers of a workg
 constexpr int kGridBins = 1024;     // 32 nats below the largest logit; weights beyond sum to less than 2^20 e^-31
 constexpr int kCopies = 4;          // of each bin, by lane, against LDS atomics on one address
 constexpr int kListCap = 4096;      // tokens of the listed bins
-constexpr int kShortList = 128;     // of them, ordered without a second look
 constexpr int kRowsPerLaunch = 1024;
 constexpr int kMaxSplits = 64;
 constexpr double kPerNat = 32.0;
@@ -335,7 +353,7 @@ struct Grid {
 };
 
 // the pieces of 16 bytes that hold a split of a row, in registers; places outside the row are -inf
-template <bool kBf16, int NV>
+template <bool kBf16, int NV, int kThreads>
 struct Pieces {
   static constexpr int kPer = kBf16 ? 8 : 4;  // tokens of a piece
   uint4 v[NV];
@@ -345,15 +363,15 @@ struct Pieces {
     const char* row = static_cast<const char*>(p.logits) + r * p.row_stride * (kBf16 ? 2 : 4);
     const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(row) % 16) / (kBf16 ? 2 : 4);
     const uint4* base = reinterpret_cast<const uint4*>(row - skew * (kBf16 ? 2 : 4));
-    const int q0 = s * kScanThreads * NV + static_cast<int>(threadIdx.x);
+    const int q0 = s * kThreads * NV + static_cast<int>(threadIdx.x);
     first = q0 * kPer - skew;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int e0 = first + i * kScanThreads * kPer;
+      const int e0 = first + i * kThreads * kPer;
       v[i] = kBf16 ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u)
                    : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
       if (e0 >= 0 && e0 + kPer <= p.V) {
-        v[i] = base[q0 + i * kScanThreads];
+        v[i] = base[q0 + i * kThreads];
       } else if (e0 + kPer > 0 && e0 < p.V) {  // the row's first or last piece
         uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
 #pragma unroll
@@ -374,7 +392,7 @@ struct Pieces {
     const uint32_t w = (kBf16 ? j / 2 : j) == 0 ? v[i].x : (kBf16 ? j / 2 : j) == 1 ? v[i].y : (kBf16 ? j / 2 : j) == 2 ? v[i].z : v[i].w;
     return __uint_as_float(kBf16 ? (j % 2 ? w & 0xffff0000u : w << 16) : w);
   }
-  __device__ __forceinline__ int index(int i, int j) const { return first + i * kScanThreads * kPer + j; }
+  __device__ __forceinline__ int index(int i, int j) const { return first + i * kThreads * kPer + j; }
   // largest logit of a piece; NaN never wins
   __device__ __forceinline__ float largest(int i) const {
     float m = -INFINITY;
@@ -416,11 +434,11 @@ template <bool kBf16, int NV>
 __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(8))) void sample_scan_kernel(
     SampleParams p, int row0, int splits) {
   __shared__ unsigned long long s_bin[kGridBins * kCopies];
-  __shared__ uint32_t s_max[kScanThreads / kWave];
+  __shared__ uint32_t s_max[2 * kScanThreads / kWave];
   __shared__ int s_part[2 * kScanThreads / kWave];
-  __shared__ int s_n;
+  __shared__ int s_n, s_queued;
   const int local = blockIdx.x / splits, r = row0 + local, s = blockIdx.x % splits, tid = threadIdx.x;
-  Pieces<kBf16, NV> z;
+  Pieces<kBf16, NV, kScanThreads> z;
   z.load(p, r, s);  // ahead of the settings
   const Mode mode = row_mode(p, r);
   const RowView ws(p, local, splits);
@@ -430,7 +448,7 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(8)
     ws.row->slow = mode == Mode::Slow;
   }
   if (mode == Mode::Slow) return;
-  if (tid == 0) s_n = 0;
+  if (tid == 0) s_n = s_queued = 0;
   if (mode == Mode::Full)
     for (int i = tid; i < kGridBins * kCopies; i += kScanThreads) s_bin[i] = 0;
   uint32_t most[NV], top = 0;
@@ -439,8 +457,8 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(8)
     most[i] = token_key(z.largest(i));
     top = max(top, most[i]);
   }
-  const uint32_t mine = top;
-  top = block_max(top, s_max);  // orders the clearing above, too
+  uint32_t low = top;  // the smallest of the threads' largest
+  block_range(top, low, s_max);  // orders the clearing above, too
   if (tid == 0) out.top = top;
   if (top <= kKeyNegInf) {
     if (tid == 0) out.n = 0;
@@ -452,7 +470,7 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(8)
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
 #pragma unroll
-      for (int j = 0; j < Pieces<kBf16, NV>::kPer; ++j) {
+      for (int j = 0; j < Pieces<kBf16, NV, kScanThreads>::kPer; ++j) {
         const double g = static_cast<double>(z.logit(i, j)) * grid.scale, b = floor(g);
         const double t = grid_top - b;
         if (t >= 0.0 && t < kGridBins) {
@@ -483,7 +501,7 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(8)
       return block_count(c, s_part, turn++);
     };
     // every thread's largest logit is at least the smallest of them, and k < kScanThreads
-    cut = max(~block_max(~mine, s_max), kKeyNegInf + 1);
+    cut = max(low, kKeyNegInf + 1);
     if (pieces(cut) >= k) cut = bisect<uint32_t>(cut, top, k, k + k / 8 + 8, pieces);
     auto tokens = [&](uint32_t least) {
       int c = 0;
@@ -491,7 +509,7 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(8)
       for (int i = 0; i < NV; ++i) {
         if (__ballot(most[i] >= least) == 0) continue;
 #pragma unroll
-        for (int j = 0; j < Pieces<kBf16, NV>::kPer; ++j) c += popc64(__ballot(token_key(z.logit(i, j)) >= least));
+        for (int j = 0; j < Pieces<kBf16, NV, kScanThreads>::kPer; ++j) c += popc64(__ballot(token_key(z.logit(i, j)) >= least));
       }
       return block_count(c, s_part, turn++);
     };
@@ -505,7 +523,7 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(8)
     for (int i = NV - 1; i >= 0; --i) {
       if (most[i] != top) continue;
 #pragma unroll
-      for (int j = Pieces<kBf16, NV>::kPer - 1; j >= 0; --j)
+      for (int j = Pieces<kBf16, NV, kScanThreads>::kPer - 1; j >= 0; --j)
         if (token_key(z.logit(i, j)) == top) best = 0xffffffffu - static_cast<uint32_t>(z.index(i, j));
     }
     best = block_max(best, s_max);
@@ -515,21 +533,37 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(8)
     }
     return;
   }
+  // The pieces that reach the cut, a few of each wave, are queued in LDS and their tokens
+  // looked at one per thread.  More pieces than the queue holds: more candidates than
+  // the list holds, too.
+  uint4* queue = reinterpret_cast<uint4*>(s_bin);
+  int* first = reinterpret_cast<int*>(queue + kCandCap);
+  static_assert(sizeof(s_bin) >= kCandCap * (sizeof(uint4) + sizeof(int)), "the queue fits");
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     if (most[i] < cut) continue;
-#pragma unroll
-    for (int j = 0; j < Pieces<kBf16, NV>::kPer; ++j) {
-      const uint32_t key = token_key(z.logit(i, j));
-      if (key >= cut) {
-        const int at = atomicAdd(&s_n, 1);
-        if (at < kCandCap) out.data[at] = token_order(key, z.index(i, j));
-      }
+    const int at = atomicAdd(&s_queued, 1);
+    if (at < kCandCap) {
+      queue[at] = z.v[i];
+      first[at] = z.index(i, 0);
+    }
+  }
+  __syncthreads();
+  constexpr int kPer = Pieces<kBf16, NV, kScanThreads>::kPer;
+  const int queued = s_queued;
+  for (int i = tid; i < min(queued, kCandCap) * kPer; i += kScanThreads) {
+    const int j = i % kPer;
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(queue + i / kPer);
+    const uint32_t bits = kBf16 ? (j % 2 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16) : w[j];
+    const uint32_t key = token_key(__uint_as_float(bits));
+    if (key >= cut) {
+      const int at = atomicAdd(&s_n, 1);
+      if (at < kCandCap) out.data[at] = token_order(key, first[i / kPer] + j);
     }
   }
   __syncthreads();
   if (tid == 0) {
-    out.n = s_n;
+    out.n = queued > kCandCap ? queued : s_n;
     out.cut = cut;
   }
 }
@@ -726,10 +760,15 @@ __device__ void wave_pick(const SampleParams& p, int r, uint32_t top, int k, uns
   }
 }
 
-// Candidates of a greedy or top-k row -> token.  False: the lists do not hold them all.
-// Up to 1024 candidates and a top_k of 256 one wave does it all in registers (a
-// workgroup with its barriers took 18 us instead); more, the workgroup.
-__device__ bool pick_candidates(const SampleParams& p, int r, Mode mode, const RowView& ws, int splits, PickShared& sh) {
+// What became of a greedy or top-k row: done, left to a workgroup, or more candidates than
+// the lists hold.
+enum class Picked { Done, Block, Slow };
+
+// Candidates of a greedy or top-k row -> token.  Up to 1024 candidates and a top_k of 256
+// the first wave does it all in registers (a workgroup with its barriers took 18 us
+// instead); more are for a workgroup of kScanThreads (kBlock).
+template <bool kBlock, class Shared>
+__device__ Picked pick_candidates(const SampleParams& p, int r, Mode mode, const RowView& ws, int splits, Shared& sh) {
   const int tid = threadIdx.x, lane = lane_id();
   // every wave reads the splits' heads, one per lane
   const int ns = lane < splits ? ws.split[lane].n : 0;
@@ -737,10 +776,10 @@ __device__ bool pick_candidates(const SampleParams& p, int r, Mode mode, const R
   for (int o = 32; o >= 1; o >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(top, o)));
   const int upto = wave_incl_scan_i32(ns);
   const int n = lane_value(upto, kWave - 1);
-  if (__ballot(ns > kCandCap) != 0 || n > kCandMax) return false;
+  if (__ballot(ns > kCandCap) != 0 || n > kCandMax) return Picked::Slow;
   if (n == 0) {
     if (tid == 0) p.token[r] = -1, p.prob[r] = 0.f;
-    return true;
+    return Picked::Done;
   }
   if (mode == Mode::Greedy) {
     if (tid < kWave) {
@@ -748,7 +787,7 @@ __device__ bool pick_candidates(const SampleParams& p, int r, Mode mode, const R
       for (int o = 32; o >= 1; o >>= 1) best = max(best, __shfl_xor(best, o));
       if (tid == 0) p.token[r] = order_index(best), p.prob[r] = 1.f;
     }
-    return true;
+    return Picked::Done;
   }
   const int k = min(p.top_k[r], n);
   // a split with k candidates of its own: at least k of the row reach its cut
@@ -760,7 +799,7 @@ __device__ bool pick_candidates(const SampleParams& p, int r, Mode mode, const R
   }
   constexpr int kWaveMine = 16, kWaveK = 256;
   if (n <= kWaveMine * kWave && k <= kWaveK) {
-    if (wave_id() != 0) return true;  // no barrier follows
+    if (kBlock || wave_id() != 0) return Picked::Done;  // no barrier follows
     wave_lds_sync();
     unsigned long long mine[kWaveMine];
 #pragma unroll
@@ -804,74 +843,116 @@ __device__ bool pick_candidates(const SampleParams& p, int r, Mode mode, const R
         wave_pick<4>(p, r, top, k, v);
       }
     }
-    return true;
+    return Picked::Done;
   }
-  __syncthreads();
-  constexpr int kMine = kCandMax / kScanThreads;
-  unsigned long long mine[kMine];
+  if constexpr (!kBlock) {
+    return Picked::Block;
+  } else {
+    __syncthreads();
+    constexpr int kMine = kCandMax / kScanThreads;
+    unsigned long long mine[kMine];
 #pragma unroll
-  for (int i = 0; i < kMine; ++i)
-    mine[i] = tid + i * kScanThreads < n ? candidate(ws, sh.offset, tid + i * kScanThreads) : 0;
-  int turn = 0;
-  const unsigned long long cut = cut_to(
-      k, least, top,
-      [&](uint32_t key) {
-        int c = 0;
+    for (int i = 0; i < kMine; ++i)
+      mine[i] = tid + i * kScanThreads < n ? candidate(ws, sh.offset, tid + i * kScanThreads) : 0;
+    int turn = 0;
+    const unsigned long long cut = cut_to(
+        k, least, top,
+        [&](uint32_t key) {
+          int c = 0;
 #pragma unroll
-        for (int i = 0; i < kMine; ++i)
-          if (i * kScanThreads < n) c += popc64(__ballot(order_key(mine[i]) >= key && mine[i] != 0));
-        return block_count(c, sh.part32, turn++);
-      },
-      [&](unsigned long long token) {
-        int c = 0;
+          for (int i = 0; i < kMine; ++i)
+            if (i * kScanThreads < n) c += popc64(__ballot(order_key(mine[i]) >= key && mine[i] != 0));
+          return block_count(c, sh.part32, turn++);
+        },
+        [&](unsigned long long token) {
+          int c = 0;
 #pragma unroll
-        for (int i = 0; i < kMine; ++i)
-          if (i * kScanThreads < n) c += popc64(__ballot(mine[i] >= token && mine[i] != 0));
-        return block_count(c, sh.part32, turn++);
-      });
-  __syncthreads();
-  if (tid == 0) sh.n = 0;
-  __syncthreads();
+          for (int i = 0; i < kMine; ++i)
+            if (i * kScanThreads < n) c += popc64(__ballot(mine[i] >= token && mine[i] != 0));
+          return block_count(c, sh.part32, turn++);
+        });
+    __syncthreads();
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kMine; ++i)
-    if (mine[i] >= cut && mine[i] != 0) sh.buf[atomicAdd(&sh.n, 1)] = mine[i];  // k in all
-  __syncthreads();
-  const unsigned long long v = tid < k ? sh.buf[tid] : 0;
-  const RowRule rule{top, key_logit(top), p.temperature ? p.temperature[r] : 1.f};
-  const Sorted t = sort_and_sum(v, k, sh.buf, sh.part, [&](uint32_t key) { return rule.weight(key); });
-  int keep = k;
-  if (p.top_p && !(p.top_p[r] >= 1.f)) {
-    const double want = fmax(static_cast<double>(p.top_p[r]), 0.0) * thread_value(t.sum, k - 1, sh);
-    keep = min(keep, first_thread(tid < k && t.sum >= want, k, sh) + 1);
+    for (int i = 0; i < kMine; ++i)
+      if (mine[i] >= cut && mine[i] != 0) sh.buf[atomicAdd(&sh.n, 1)] = mine[i];  // k in all
+    __syncthreads();
+    const unsigned long long v = tid < k ? sh.buf[tid] : 0;
+    const RowRule rule{top, key_logit(top), p.temperature ? p.temperature[r] : 1.f};
+    const Sorted t = sort_and_sum(v, k, sh.buf, sh.part, [&](uint32_t key) { return rule.weight(key); });
+    int keep = k;
+    if (p.top_p && !(p.top_p[r] >= 1.f)) {
+      const double want = fmax(static_cast<double>(p.top_p[r]), 0.0) * thread_value(t.sum, k - 1, sh);
+      keep = min(keep, first_thread(tid < k && t.sum >= want, k, sh) + 1);
+    }
+    if (p.min_p && p.min_p[r] > 0.f)
+      keep = min(keep, first_thread(tid >= k || t.weight < fmin(static_cast<double>(p.min_p[r]), 1.0), k, sh));
+    keep = max(keep, 1);
+    const double total = thread_value(t.sum, keep - 1, sh);
+    const double at = row_uniform(p, r) * total;
+    if (tid == first_thread(tid < keep && t.sum > at, keep - 1, sh)) {
+      p.token[r] = order_index(t.token);
+      p.prob[r] = static_cast<float>(t.weight / total);
+    }
+    return Picked::Done;
   }
-  if (p.min_p && p.min_p[r] > 0.f)
-    keep = min(keep, first_thread(tid >= k || t.weight < fmin(static_cast<double>(p.min_p[r]), 1.0), k, sh));
-  keep = max(keep, 1);
-  const double total = thread_value(t.sum, keep - 1, sh);
-  const double at = row_uniform(p, r) * total;
-  if (tid == first_thread(tid < keep && t.sum > at, keep - 1, sh)) {
-    p.token[r] = order_index(t.token);
-    p.prob[r] = static_cast<float>(t.weight / total);
-  }
-  return true;
 }
 
+constexpr int kFilterThreads = 256;
+constexpr int kFilterMine = kGridBins / kFilterThreads;  // neighbouring bins of a thread
+
+struct FilterShared {
+  unsigned long long buf[256];
+  double part[kFilterThreads / kWave];
+  double value;
+  int offset[kMaxSplits + 1];
+  int at, n_cut, n_pick, cut0, pick0;
+};
+
+// smallest bin at which `hit` holds, n if none
+__device__ __forceinline__ int first_bin(const bool (&hit)[kFilterMine], int n, FilterShared& sh) {
+  int mine = n;
+#pragma unroll
+  for (int e = kFilterMine - 1; e >= 0; --e) mine = hit[e] ? static_cast<int>(threadIdx.x) * kFilterMine + e : mine;
+  const uint64_t m = __ballot(mine < n);
+  __syncthreads();
+  if (threadIdx.x == 0) sh.at = n;
+  __syncthreads();
+  if (m != 0 && lane_id() == __builtin_ctzll(m)) atomicMin(&sh.at, mine);
+  __syncthreads();
+  return sh.at;
+}
+
+__device__ __forceinline__ double bin_value(const double (&v)[kFilterMine], int bin, FilterShared& sh) {
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < kFilterMine; ++e)
+    if (static_cast<int>(threadIdx.x) * kFilterMine + e == bin) sh.value = v[e];
+  __syncthreads();
+  return sh.value;
+}
+
+// Workgroup b takes row b % rows, part b / rows: the parts that do a whole top-k row come
+// first and go to all XCDs in turn (workgroup b runs on XCD b % 8; with a row's parts side
+// by side they fell on two of them, 132 us of 512 x 100003).
 template <bool kBf16, int NV>
-__global__ __launch_bounds__(kScanThreads) void sample_filter_kernel(SampleParams p, int row0, int splits) {
-  __shared__ PickShared sh;
-  __shared__ int s_cut, s_pick, s_cut0, s_pick0;
-  const int local = blockIdx.x / splits, r = row0 + local, s = blockIdx.x % splits, tid = threadIdx.x;
+__global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SampleParams p, int row0, int rows, int splits) {
+  __shared__ FilterShared sh;
+  const int local = blockIdx.x % rows, r = row0 + local, s = blockIdx.x / rows, tid = threadIdx.x;
   const Mode mode = row_mode(p, r);
   const RowView ws(p, local, splits);
   if (mode == Mode::Slow) return;
   if (mode != Mode::Full) {
-    if (s == 0 && !pick_candidates(p, r, mode, ws, splits, sh) && tid == 0) ws.row->slow = 1;
+    if (s != 0) return;
+    const Picked done = pick_candidates<false>(p, r, mode, ws, splits, sh);
+    if (tid == 0 && done != Picked::Done) ws.row->slow = done == Picked::Slow ? 1 : 2;
     return;
   }
-  Pieces<kBf16, NV> z;
+  Pieces<kBf16, NV, kFilterThreads> z;
   z.load(p, r, s);  // needed last, requested first
-  uint32_t top = 0;
-  for (int i = 0; i < splits; ++i) top = max(top, ws.split[i].top);
+  uint32_t top = lane_id() < splits ? ws.split[lane_id()].top : 0;
+  for (int o = 32; o >= 1; o >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(top, o)));
   const double tau = p.temperature ? static_cast<double>(p.temperature[r]) : 1.0;
   const Grid grid{kPerNat / tau};
   const double grid_top = floor(grid.at(top));
@@ -883,40 +964,68 @@ __global__ __launch_bounds__(kScanThreads) void sample_filter_kernel(SampleParam
     ws.row->grid_top = grid_top;
   }
   if (top <= kKeyNegInf || slow) return;
-  // thread t: the row's sum in bin t below its largest logit
-  unsigned long long sum = 0;
+  // the row's sums in this thread's bins below its largest logit
+  unsigned long long sum[kFilterMine] = {};
   for (int i = 0; i < splits; ++i) {
     const uint32_t part_top = ws.split[i].top;
     if (part_top <= kKeyNegInf) continue;
-    const double at = tid - (grid_top - floor(grid.at(part_top)));
-    if (at >= 0.0) sum += ws.split[i].data[static_cast<int>(at)];
+    const double lower = grid_top - floor(grid.at(part_top));
+    if (lower >= kGridBins) continue;
+    const int at = tid * kFilterMine - static_cast<int>(lower);
+#pragma unroll
+    for (int e = 0; e < kFilterMine; ++e)
+      if (at + e >= 0) sum[e] += ws.split[i].data[at + e];
   }
-  const double w = static_cast<double>(sum) / kWeightOne * exp(-tid / kPerNat);
-  const double incl = block_scan(w, sh.part), excl = incl - w;
-  const double total = thread_value(incl, kScanThreads - 1, sh);
+  double incl[kFilterMine], excl[kFilterMine], mine = 0.0;
+  const double base = exp(-tid * kFilterMine / kPerNat) / kWeightOne;
+  constexpr double kStep = 0.96923323447634413;  // exp(-1 / 32)
+  double factor = base;
+#pragma unroll
+  for (int e = 0; e < kFilterMine; ++e) {
+    excl[e] = mine;
+    mine += static_cast<double>(sum[e]) * factor;
+    incl[e] = mine;
+    factor *= kStep;
+  }
+  const double front = block_scan(mine, sh.part) - mine;
+#pragma unroll
+  for (int e = 0; e < kFilterMine; ++e) {
+    excl[e] += front;
+    incl[e] += front;
+  }
+  const double total = bin_value(incl, kGridBins - 1, sh);
+  bool hit[kFilterMine];
+  auto first = [&](auto passes, int n) {
+#pragma unroll
+    for (int e = 0; e < kFilterMine; ++e) hit[e] = passes(incl[e]);
+    return min(first_bin(hit, n, sh), n);
+  };
   int cut = -1;
   double kept = total, least = total;  // the kept sum lies between
   if (p.top_p && !(p.top_p[r] >= 1.f)) {
     const double want = fmax(static_cast<double>(p.top_p[r]), 0.0) * total;
-    cut = min(first_thread(incl >= want, kScanThreads - 1, sh), kScanThreads - 1);
+    cut = first([&](double v) { return v >= want; }, kGridBins - 1);
   }
   if (p.min_p && p.min_p[r] > 0.f) {
     const double m = fmin(static_cast<double>(p.min_p[r]), 1.0);
     const double t = grid_top - floor(grid.at(top) + kPerNat * log(m));
-    if (t < (cut < 0 ? kScanThreads : cut)) cut = static_cast<int>(t);
+    if (t < (cut < 0 ? kGridBins : cut)) cut = static_cast<int>(t);
   }
   if (cut >= 0) {
-    kept = thread_value(incl, cut, sh);
-    least = thread_value(excl, cut, sh);
+    kept = bin_value(incl, cut, sh);
+    least = bin_value(excl, cut, sh);
   }
   const double u = row_uniform(p, r);
   // the last bin that holds a kept weight, for roundings at the end
-  const int last = cut >= 0 ? cut : first_thread(incl >= total, kScanThreads - 1, sh);
-  const int pick0 = min(first_thread(incl > u * least, last, sh), last);
-  const int pick1 = min(first_thread(incl > u * kept, last, sh), last);
+  const int last = cut >= 0 ? cut : first([&](double v) { return v >= total; }, kGridBins - 1);
+  const int pick0 = first([&](double v) { return v > u * least; }, last);
+  const int pick1 = kept > least ? first([&](double v) { return v > u * kept; }, last) : pick0;
   if (s == 0) {
-    if (tid == pick0) ws.row->before_pick = excl;
-    if (tid == cut) ws.row->before_cut = excl;
+#pragma unroll
+    for (int e = 0; e < kFilterMine; ++e) {
+      if (tid * kFilterMine + e == pick0) ws.row->before_pick = excl[e];
+      if (tid * kFilterMine + e == cut) ws.row->before_cut = excl[e];
+    }
     if (tid == 0) {
       ws.row->t_cut = cut;
       ws.row->t_pick0 = pick0;
@@ -926,7 +1035,7 @@ __global__ __launch_bounds__(kScanThreads) void sample_filter_kernel(SampleParam
   }
   // which of this thread's tokens lie in those bins (32 tokens at most), then room for
   // them: one counter per list in LDS, one addition to the row's per workgroup
-  constexpr int kPer = Pieces<kBf16, NV>::kPer;
+  constexpr int kPer = Pieces<kBf16, NV, kFilterThreads>::kPer;
   static_assert(NV * kPer <= 32, "a bit per token");
   uint32_t in_cut = 0, in_pick = 0;
 #pragma unroll
@@ -938,18 +1047,18 @@ __global__ __launch_bounds__(kScanThreads) void sample_filter_kernel(SampleParam
       in_pick |= t >= pick0 && t <= pick1 ? 1u << (i * kPer + j) : 0u;
     }
   }
-  if (tid == 0) s_cut = s_pick = 0;
+  if (tid == 0) sh.n_cut = sh.n_pick = 0;
   __syncthreads();
-  int at_cut = in_cut ? atomicAdd(&s_cut, __popc(in_cut)) : 0;
-  int at_pick = in_pick ? atomicAdd(&s_pick, __popc(in_pick)) : 0;
+  int at_cut = in_cut ? atomicAdd(&sh.n_cut, __popc(in_cut)) : 0;
+  int at_pick = in_pick ? atomicAdd(&sh.n_pick, __popc(in_pick)) : 0;
   __syncthreads();
   if (tid == 0) {
-    s_cut0 = s_cut ? atomicAdd(&ws.row->n_cut, s_cut) : 0;
-    s_pick0 = s_pick ? atomicAdd(&ws.row->n_pick, s_pick) : 0;
+    sh.cut0 = sh.n_cut ? atomicAdd(&ws.row->n_cut, sh.n_cut) : 0;
+    sh.pick0 = sh.n_pick ? atomicAdd(&ws.row->n_pick, sh.n_pick) : 0;
   }
   __syncthreads();
-  at_cut += s_cut0;
-  at_pick += s_pick0;
+  at_cut += sh.cut0;
+  at_pick += sh.pick0;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
 #pragma unroll
@@ -974,53 +1083,132 @@ union FinishShared {
   PickShared pick;
 };
 
-// The tokens around one place of a listed range of bins, one per thread.
-struct Near {
-  unsigned long long token;  // of this thread; 0 from n on
-  int n;
-  double before;  // weights of the row in front of them
+// A listed range of bins in a workgroup's registers: token and weight, in 2^-43 of the
+// range's first bin (whole numbers: sums in any order are the same).
+struct Listed {
+  static constexpr int kMine = kListCap / kScanThreads;
+  unsigned long long token[kMine], weight[kMine];
+  double unit;  // what 1 of them stands for
+
+  __device__ __forceinline__ Listed(const unsigned long long* list, int n, const Grid& grid, double grid_top, int t0)
+      : unit(exp(-t0 / kPerNat) / kWeightOne) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      token[i] = weight[i] = 0;
+      const int at = static_cast<int>(threadIdx.x) + i * kScanThreads;
+      if (at >= n) continue;
+      token[i] = list[at];
+      const double g = grid.at(order_key(token[i])), b = floor(g);
+      weight[i] = __double2ull_rn(Grid::weight(g - b) * exp((b + t0 - grid_top) / kPerNat) * kWeightOne);
+    }
+  }
 };
 
-// From a list of n <= kListCap tokens in `bins` bins from bin t0 on, those around the place
-// where passes(running sum) turns true, or of finer bin `limit` if that comes first.
-// A list of up to kShortList is taken as it is (sorting 1024 takes 10 us, 128 2 us); a longer one is
-// cut into kScanThreads finer bins, whose sums are whole numbers, too.  n > kScanThreads: too many (equal logits).
+struct Sums {
+  unsigned long long weight;
+  int count;
+};
+
+// Workgroup-wide sums; one barrier a call, calls in a row alternate between two halves.
+__device__ __forceinline__ Sums block_sums(unsigned long long w, int c, PickShared& sh, int turn) {
+  constexpr int kWaves = kScanThreads / kWave;
+  for (int o = 32; o >= 1; o >>= 1) w += __shfl_xor(w, o);
+  if (lane_id() == 0) {
+    sh.fine[(turn & 1) * kWaves + wave_id()] = w;
+    sh.part32[(turn & 1) * kWaves + wave_id()] = c;
+  }
+  __syncthreads();
+  unsigned long long v = sh.fine[(turn & 1) * kWaves + lane_id() % kWaves];
+  for (int o = kWaves / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o);
+  return {v, wave_sum_i32(sh.part32[(turn & 1) * kWaves + lane_id() % kWaves]) / (kWave / kWaves)};
+}
+
+// The token of a list at which passes(before + sum up to it) turns true, and that sum; the
+// list's last one if it never does.  The order is searched by halves until at most 64 tokens
+// are left around the place, and those are sorted by every wave for itself.
+struct PlaceInList {
+  unsigned long long token;
+  double sum;
+};
 template <class Passes>
-__device__ __forceinline__ Near tokens_near(const unsigned long long* list, int n, const Grid& grid, double grid_top,
-                                            int t0, int bins, double before, int limit, PickShared& sh, Passes passes) {
-  const int tid = threadIdx.x;
-  if (n <= kShortList) return {tid < n ? list[tid] : 0, n, before};
-  constexpr int kMine = kListCap / kScanThreads;
-  unsigned long long* fine = sh.fine;
-  __syncthreads();
-  fine[tid] = 0;
-  if (tid == 0) sh.n = 0;
-  __syncthreads();
-  int sub[kMine];
+__device__ __forceinline__ PlaceInList place_in_list(const Listed& l, int n, double before, PickShared& sh, Passes passes) {
+  unsigned long long lo = 1, hi = ~0ull;  // tokens in [lo, hi): the place and its neighbours
+  Sums above = {0, 0};                    // of tokens from hi on
+  int inside = n, turn = 0;
+  // every token lies in [least, most]: a list's keys share their upper bits
+  unsigned long long least = ~0ull, most = 0;
 #pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    sub[i] = -1;
-    if (tid + i * kScanThreads >= n) continue;
-    const double g = grid.at(order_key(list[tid + i * kScanThreads])), b = floor(g);
-    // the bin's own tokens run from its top (rest near 1) down
-    const double place = (grid_top - b - t0 + (1.0 - (g - b))) * (kScanThreads / static_cast<double>(bins));
-    sub[i] = min(max(static_cast<int>(place), 0), kScanThreads - 1);
-    const double w = Grid::weight(g - b) * exp((b + t0 - grid_top) / kPerNat);
-    atomicAdd(&fine[sub[i]], static_cast<unsigned long long>(__double2ull_rn(w * kWeightOne)));
+  for (int i = 0; i < Listed::kMine; ++i) {
+    if (l.token[i] == 0) continue;
+    least = min(least, l.token[i]);
+    most = max(most, l.token[i]);
+  }
+  for (int o = 32; o >= 1; o >>= 1) {
+    least = min(least, __shfl_xor(least, o));
+    most = max(most, __shfl_xor(most, o));
   }
   __syncthreads();
-  const double w = static_cast<double>(fine[tid]) / kWeightOne * exp(-t0 / kPerNat);
-  const double incl = before + block_scan(w, sh.part);
-  const int at = min(first_thread(passes(incl), kScanThreads - 1, sh), limit);
-  const double front = thread_value(incl - w, at, sh);
-#pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    if (sub[i] != at) continue;
-    const int k = atomicAdd(&sh.n, 1);
-    if (k < kScanThreads) sh.buf[k] = list[tid + i * kScanThreads];
+  if (lane_id() == 0) {
+    sh.buf[wave_id()] = least;
+    sh.buf[kScanThreads / kWave + wave_id()] = most;
   }
   __syncthreads();
-  return {tid < sh.n ? sh.buf[tid] : 0, sh.n, front};
+  for (int w = 0; w < kScanThreads / kWave; ++w) {
+    least = min(least, sh.buf[w]);
+    most = max(most, sh.buf[kScanThreads / kWave + w]);
+  }
+  lo = least;
+  hi = most + 1;
+  while (inside > kWave && hi - lo > 1) {
+    const unsigned long long mid = lo + (hi - lo) / 2;
+    unsigned long long w = 0;
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < Listed::kMine; ++i) {
+      w += l.token[i] >= mid ? l.weight[i] : 0;
+      c += popc64(__ballot(l.token[i] >= mid));
+    }
+    const Sums s = block_sums(w, c, sh, turn++);
+    if (passes(before + static_cast<double>(s.weight) * l.unit)) {
+      lo = mid;
+      inside = s.count - above.count;
+    } else {
+      hi = mid;
+      inside -= s.count - above.count;
+      above = s;
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) sh.n = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < Listed::kMine; ++i) {
+    if (l.token[i] < lo || l.token[i] >= hi) continue;
+    const int at = atomicAdd(&sh.n, 1);  // 64 at most
+    sh.buf[at] = l.token[i];
+    sh.fine[at] = l.weight[i];
+  }
+  __syncthreads();
+  const int lane = lane_id(), m = sh.n;
+  unsigned long long v = lane < m ? sh.buf[lane] : 0, w = lane < m ? sh.fine[lane] : 0;
+#pragma unroll
+  for (int run = 2; run <= kWave; run *= 2) {
+#pragma unroll
+    for (int j = run / 2; j > 0; j /= 2) {
+      const unsigned long long o = __shfl_xor(v, j), ow = __shfl_xor(w, j);
+      const bool take = (((lane & run) == 0) == ((lane & j) == 0)) != (v > o);
+      v = take ? o : v;
+      w = take ? ow : w;
+    }
+  }
+  for (int o = 1; o < kWave; o <<= 1) {
+    const unsigned long long u = __shfl_up(w, o);
+    if (lane >= o) w += u;
+  }
+  const double sum = before + static_cast<double>(above.weight + w) * l.unit;
+  const uint64_t hit = __ballot(lane < m && passes(sum));
+  const int at = hit != 0 ? __builtin_ctzll(hit) : max(m - 1, 0);
+  return {__shfl(v, at), __shfl(sum, at)};
 }
 
 template <bool kBf16>
@@ -1029,6 +1217,10 @@ __global__ __launch_bounds__(kRowThreads) void sample_finish_kernel(SampleParams
   const int local = blockIdx.x, r = row0 + local, tid = threadIdx.x;
   const RowView ws(p, local, splits);
   const RowPart& in = *ws.row;
+  if (in.slow == 2) {
+    pick_candidates<true>(p, r, Mode::TopK, ws, splits, un.pick);
+    return;
+  }
   if (in.slow) {
     sample_row<kBf16>(p, r, un.row);
     return;
@@ -1040,54 +1232,43 @@ __global__ __launch_bounds__(kRowThreads) void sample_finish_kernel(SampleParams
     return;
   }
   const int n_cut = in.t_cut >= 0 ? in.n_cut : 0, n_pick = in.n_pick;
-  bool fits = n_cut <= kListCap && n_pick <= kListCap;
+  if (n_cut > kListCap || n_pick > kListCap) {
+    sample_row<kBf16>(p, r, un.row);
+    return;
+  }
   PickShared& sh = un.pick;
   const double tau = p.temperature ? static_cast<double>(p.temperature[r]) : 1.0;
   const Grid grid{kPerNat / tau};
   const double grid_top = in.grid_top;
-  auto weight = [&](uint32_t key) {
-    const double g = grid.at(key), b = floor(g);
-    return Grid::weight(g - b) * exp((b - grid_top) / kPerNat);
-  };
   double total = in.total;
-  if (fits && in.t_cut >= 0) {
-    const bool by_p = p.top_p && !(p.top_p[r] >= 1.f), by_m = p.min_p && p.min_p[r] > 0.f;
-    const double want = by_p ? fmax(static_cast<double>(p.top_p[r]), 0.0) * total : INFINITY;
-    const double m = by_m ? fmin(static_cast<double>(p.min_p[r]), 1.0) : 0.0;
-    int limit = kScanThreads - 1;
-    if (by_m) {  // the finer bin of the smallest weight that min_p keeps
-      const double place = grid_top + 1.0 - in.t_cut - (grid.at(top) + kPerNat * log(m));
-      limit = static_cast<int>(fmin(fmax(place * kScanThreads, 0.0), static_cast<double>(limit)));
+  if (in.t_cut >= 0) {
+    // both filters keep a prefix: the shorter one
+    const Listed l(in.cut, n_cut, grid, grid_top, in.t_cut);
+    double kept = INFINITY;
+    if (p.top_p && !(p.top_p[r] >= 1.f)) {
+      const double want = fmax(static_cast<double>(p.top_p[r]), 0.0) * total;
+      const PlaceInList at = place_in_list(l, n_cut, in.before_cut, sh, [&](double sum) { return sum >= want; });
+      if (at.sum >= want) kept = at.sum;
     }
-    const Near near = tokens_near(in.cut, n_cut, grid, grid_top, in.t_cut, 1, in.before_cut, limit, sh,
-                                  [&](double sum) { return sum >= want; });
-    fits = near.n <= kScanThreads;
-    if (fits) {
+    if (p.min_p && p.min_p[r] > 0.f) {
       const RowRule rule{top, key_logit(top), tau};
-      const Sorted t = sort_and_sum(near.token, near.n, sh.buf, sh.part, weight);
-      int keep = near.n;
-      if (by_p) keep = min(keep, first_thread(tid < keep && near.before + t.sum >= want, near.n, sh) + 1);
-      if (by_m)
-        keep = min(keep, first_thread(tid >= near.n || rule.weight(order_key(t.token)) < m, near.n, sh));
-      total = near.before + (keep > 0 ? thread_value(t.sum, keep - 1, sh) : 0.0);
+      const double m = fmin(static_cast<double>(p.min_p[r]), 1.0);
+      unsigned long long w = 0;
+#pragma unroll
+      for (int i = 0; i < Listed::kMine; ++i)
+        if (l.token[i] != 0 && rule.weight(order_key(l.token[i])) >= m) w += l.weight[i];
+      __syncthreads();
+      kept = fmin(kept, in.before_cut + static_cast<double>(block_sums(w, 0, sh, 0).weight) * l.unit);
     }
+    total = fmin(kept, total);
   }
-  if (fits) {
-    const double at = row_uniform(p, r) * total;
-    const Near near = tokens_near(in.pick, n_pick, grid, grid_top, in.t_pick0, in.t_pick1 - in.t_pick0 + 1,
-                                  in.before_pick, kScanThreads - 1, sh, [&](double sum) { return sum > at; });
-    fits = near.n <= kScanThreads;
-    if (fits) {
-      const Sorted t = sort_and_sum(near.token, near.n, sh.buf, sh.part, weight);
-      if (tid == first_thread(tid < near.n && near.before + t.sum > at, near.n - 1, sh)) {
-        p.token[r] = order_index(t.token);
-        p.prob[r] = static_cast<float>(t.weight / total);
-      }
-    }
-  }
-  if (!fits) {
-    __syncthreads();
-    sample_row<kBf16>(p, r, un.row);
+  const double at = row_uniform(p, r) * total;
+  const Listed l(in.pick, n_pick, grid, grid_top, in.t_pick0);
+  const PlaceInList j = place_in_list(l, n_pick, in.before_pick, sh, [&](double sum) { return sum > at; });
+  if (tid == 0) {
+    const double g = grid.at(order_key(j.token)), b = floor(g);
+    p.token[r] = order_index(j.token);
+    p.prob[r] = static_cast<float>(Grid::weight(g - b) * exp((b - grid_top) / kPerNat) / total);
   }
 }
 
@@ -1110,7 +1291,8 @@ hipError_t launch_sample_nv(const SampleParams& p, int splits, hipStream_t strea
   for (int row0 = 0; row0 < p.R; row0 += kRowsPerLaunch) {
     const int rows = p.R - row0 < kRowsPerLaunch ? p.R - row0 : kRowsPerLaunch;
     sample_scan_kernel<kBf16, NV><<<rows * splits, kScanThreads, 0, stream>>>(p, row0, splits);
-    sample_filter_kernel<kBf16, NV><<<rows * splits, kScanThreads, 0, stream>>>(p, row0, splits);
+    sample_filter_kernel<kBf16, NV><<<rows * splits * (kScanThreads / kFilterThreads), kFilterThreads, 0, stream>>>(
+        p, row0, rows, splits);
     sample_finish_kernel<kBf16><<<rows, kRowThreads, 0, stream>>>(p, row0, splits);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
