@@ -80,7 +80,7 @@ extern "C" {
 #define ACCEPTMOE_MAX_TOPK 32
 #define ACCEPTMOE_MAX_TREES 256
 #define ACCEPTMOE_MAX_TREE_NODES 1024
-#define ACCEPTMOE_MAX_VOCAB (1 << 20)
+#define ACCEPTMOE_MAX_VOCAB 1000000
 #define ACCEPTMOE_MAX_SAMPLE_ROWS (1 << 20)
 /* static scratch of acceptmoe_select_noalloc per device: 8 MiB (e.g. up to
  * 7,000 nodes at E = 128, k = 8; acceptmoe_select_workspace_size gives the need) */

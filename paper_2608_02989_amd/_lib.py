@@ -34,7 +34,7 @@ MAX_EXPERTS = 512
 MAX_TOPK = 32
 MAX_TREES = 256
 MAX_TREE_NODES = 1024
-MAX_VOCAB = 1 << 20
+MAX_VOCAB = 1000000
 MAX_SAMPLE_ROWS = 1 << 20
 SELECT_NOALLOC_MAX_WORKSPACE = 8 << 20
 

@@ -125,7 +125,7 @@ struct AcceptParams {
 hipError_t launch_accept(const AcceptParams& p, const TreeOffsets& offs, int max_nodes, hipStream_t stream);
 
 // ---- sampling (sample.hip) ----
-constexpr int kMaxVocab = 1 << 20;
+constexpr int kMaxVocab = 1000000;
 
 struct SampleParams {
   const void* logits;

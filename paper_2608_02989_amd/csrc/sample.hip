@@ -65,9 +65,33 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* part) {
   return s;
 }
 
-// u as used: in [0, 1)
-__device__ __forceinline__ double row_uniform(const SampleParams& p, int r) {
-  return fmin(fmax(static_cast<double>(p.uniform[r]), 0.0), 1.0 - 1.0 / 16777216.0);
+constexpr int kFastK = 1000;  // largest top_k taken by candidate lists: one sorted candidate per thread
+
+enum class Mode { Greedy, TopK, Full, Slow };
+
+// A row's settings.  Absent ones are read from `uniform` and replaced, so that all loads
+// go out together and no branch waits for one.
+struct Rules {
+  float tau;
+  int k;
+  double top_p, min_p, u;  // top_p >= 1, min_p <= 0: off
+  Mode mode;
+  __device__ __forceinline__ bool by_p() const { return !(top_p >= 1.0); }
+  __device__ __forceinline__ bool by_m() const { return min_p > 0.0; }
+};
+__device__ __forceinline__ Rules row_rules(const SampleParams& p, int r) {
+  const float tau = (p.temperature ? p.temperature : p.uniform)[r];
+  const int k = (p.top_k ? p.top_k : reinterpret_cast<const int32_t*>(p.uniform))[r];
+  const float top_p = (p.top_p ? p.top_p : p.uniform)[r], min_p = (p.min_p ? p.min_p : p.uniform)[r];
+  const float u = p.uniform[r];
+  Rules s;
+  s.tau = p.temperature ? tau : 1.f;
+  s.k = p.top_k ? k : 0;
+  s.top_p = p.top_p ? fmax(static_cast<double>(top_p), 0.0) : 1.0;
+  s.min_p = p.min_p ? fmin(static_cast<double>(min_p), 1.0) : 0.0;
+  s.u = fmin(fmax(static_cast<double>(u), 0.0), 1.0 - 1.0 / 16777216.0);
+  s.mode = !(s.tau > 0.f) ? Mode::Greedy : s.k <= 0 || s.k >= p.V ? Mode::Full : s.k <= kFastK ? Mode::TopK : Mode::Slow;
+  return s;
 }
 
 // the workgroup's largest `high` and smallest `low`
@@ -191,7 +215,7 @@ __device__ int find_index(const Row<kBf16>& row, uint32_t key, uint64_t r, RowSh
 }
 
 template <bool kBf16>
-__device__ void sample_row(const SampleParams& p, int r, RowShared& sh) {
+__device__ void sample_row(const SampleParams& p, int r, const Rules& rules, RowShared& sh) {
   const int tid = threadIdx.x;
   const Row<kBf16> row{static_cast<const char*>(p.logits) + r * p.row_stride * (kBf16 ? 2 : 4), p.V};
   uint32_t top = 0;
@@ -201,17 +225,16 @@ __device__ void sample_row(const SampleParams& p, int r, RowShared& sh) {
     if (tid == 0) p.token[r] = -1, p.prob[r] = 0.f;
     return;
   }
-  const float tau = p.temperature ? p.temperature[r] : 1.f;
-  if (!(tau > 0.f)) {  // greedy
+  if (rules.mode == Mode::Greedy) {
     const int i = find_index(row, top, 1, sh);
     if (tid == 0) p.token[r] = i, p.prob[r] = 1.f;
     return;
   }
-  const RowRule rule{top, key_logit(top), tau};
+  const RowRule rule{top, key_logit(top), rules.tau};
   // top-k: tokens above (cut, ties of it)
   uint32_t cut = 0;
   uint64_t ties = 0;
-  const int k = p.top_k ? p.top_k[r] : 0;
+  const int k = rules.k;
   if (k > 0 && k < p.V) {
     uint32_t live = 0;
     for (int i = tid; i < p.V; i += kRowThreads) live += row.key(i) > kKeyNegInf ? 1u : 0u;
@@ -231,26 +254,24 @@ __device__ void sample_row(const SampleParams& p, int r, RowShared& sh) {
     return block_sum(s, sh.part64);
   };
   uint64_t total = sum_above(max(cut, kKeyNegInf)) + (cut != 0 ? ties * rule.fixed(cut) : 0);
-  const float top_p = p.top_p ? p.top_p[r] : 1.f;
-  if (!(top_p >= 1.f)) {
-    const double want = ceil(static_cast<double>(top_p > 0.f ? top_p : 0.f) * static_cast<double>(total));
+  if (rules.by_p()) {
+    const double want = ceil(rules.top_p * static_cast<double>(total));
     const uint64_t need = min(max(static_cast<uint64_t>(want), static_cast<uint64_t>(1)), total);
     const Place at = find_place<kBf16, false>(row, rule, need, sh);
     const uint64_t w = rule.fixed(at.key);
     cut = at.key;
     total = at.before + (need - at.before + w - 1) / w * w;
   }
-  const double min_p = p.min_p ? fmin(static_cast<double>(p.min_p[r]), 1.0) : 0.0;
-  if (min_p > 0.0 && (cut == 0 || rule.weight(cut) < min_p)) {
+  if (rules.by_m() && (cut == 0 || rule.weight(cut) < rules.min_p)) {
     // tokens that weigh less come behind all others
     unsigned long long s = 0;
     for (int i = tid; i < p.V; i += kRowThreads) {
       const uint32_t key = row.key(i);
-      if (key > max(cut, kKeyNegInf) && rule.weight(key) >= min_p) s += rule.fixed(key);
+      if (key > max(cut, kKeyNegInf) && rule.weight(key) >= rules.min_p) s += rule.fixed(key);
     }
     total = block_sum(s, sh.part64);
   }
-  const uint64_t need = min(static_cast<uint64_t>(row_uniform(p, r) * static_cast<double>(total)) + 1, total);
+  const uint64_t need = min(static_cast<uint64_t>(rules.u * static_cast<double>(total)) + 1, total);
   const Place at = find_place<kBf16, false>(row, rule, need, sh);
   const uint64_t w = rule.fixed(at.key);
   const int i = find_index(row, at.key, (need - at.before + w - 1) / w, sh);
@@ -262,29 +283,28 @@ __device__ void sample_row(const SampleParams& p, int r, RowShared& sh) {
 
 
 // ---------------------------------------------------------------------------
-// The common cases in three launches that read a row once or twice, R x splits
-// workgroups wide.  What each does depends on the row's settings:
+// The common cases, rows spread over R x splits workgroups.  What a launch does depends on
+// the row's settings:
 //   greedy, or 0 < top_k <= kFastK: `scan` lists each split's candidates (the largest
-//     logits, at least top_k of them), `filter` (one workgroup of the row) cuts
-//     them to the top_k, sorts those and picks.
-//   no top_k: `scan` sums weights per bin of 1/32 in z / temperature, `filter` finds the
-//     bins in which the kept prefix ends and in which the sample lies, and lists
-//     the tokens of those, `finish` orders them and picks.
+//     logits, at least top_k of them), `place` cuts them to the top_k, sorts those and
+//     picks.  One read of the row.
+//   no top_k: `scan` sums weights per bin of 1/32 in z / temperature, `place` finds the
+//     bins in which the kept prefix ends and in which the sample lies, `filter` lists
+//     the tokens of those (the second read), `finish` orders them and picks.
 //   other top_k, more candidates or tokens in a bin than the lists hold (many
 //     equal logits): `finish` runs sample_row.
 // ---------------------------------------------------------------------------
-constexpr int kScanThreads = 1024;
-constexpr int kFastK = 1000;        // one sorted candidate per thread
+constexpr int kScanThreads = 512;    // four workgroups per CU, in different phases
+constexpr int kBlockThreads = 1024;
 constexpr int kCandCap = 1280;      // candidates of a split
-constexpr int kCandMax = 8192;      // candidates of a row (registers of a workgroup)
+constexpr int kCandMax = 16384;     // candidates of a row (registers of a workgroup)
 constexpr int kGridBins = 1024;     // 32 nats below the largest logit; weights beyond sum to less than 2^20 e^-31
 constexpr int kCopies = 4;          // of each bin, by lane, against LDS atomics on one address
 constexpr int kListCap = 4096;      // tokens of the listed bins
+constexpr int kWaveList = 1024;     // of them, as many as one wave handles
 constexpr int kRowsPerLaunch = 1024;
 constexpr int kMaxSplits = 64;
 constexpr double kPerNat = 32.0;
-
-enum class Mode { Greedy, TopK, Full, Slow };
 
 // a token as one number: larger logit, then lower index, is larger
 __device__ __forceinline__ unsigned long long token_order(uint32_t key, int index) {
@@ -303,13 +323,15 @@ struct SplitPart {
 };
 static_assert(kGridBins <= kCandCap, "bins fit");
 
-struct RowPart {
+struct RowHead {
   int n_cut, n_pick;     // tokens listed (may exceed kListCap)
   int t_cut;             // bin in which the kept prefix ends, -1: everything is kept
   int t_pick0, t_pick1;  // bins in which the sample lies
   int slow;              // finish with sample_row
   uint32_t top;
   double before_cut, before_pick, total, grid_top;
+};
+struct RowPart : RowHead {
   unsigned long long cut[kListCap], pick[kListCap];
 };
 
@@ -326,13 +348,6 @@ struct RowView {
     split = reinterpret_cast<SplitPart*>(base + sizeof(RowPart));
   }
 };
-
-__device__ __forceinline__ Mode row_mode(const SampleParams& p, int r) {
-  if (p.temperature && !(p.temperature[r] > 0.f)) return Mode::Greedy;
-  const int k = p.top_k ? p.top_k[r] : 0;
-  if (k <= 0 || k >= p.V) return Mode::Full;
-  return k <= kFastK ? Mode::TopK : Mode::Slow;
-}
 
 // z / temperature in bins of 1/32: the whole part names the bin, the rest gives the
 // weight within it, exp(rest / 32) in [1, 1.032).  A bin's sum of these does not depend
@@ -404,8 +419,9 @@ struct Pieces {
 
 // Workgroup-wide number of the values a thread counts by ballot; one barrier a call,
 // calls in a row alternate between two halves of `part`.
+template <int kThreads>
 __device__ __forceinline__ int block_count(int wave_count, int* part, int turn) {
-  constexpr int kWaves = kScanThreads / kWave;
+  constexpr int kWaves = kThreads / kWave;
   int* half = part + (turn & 1) * kWaves;
   if (lane_id() == 0) half[wave_id()] = wave_count;
   __syncthreads();
@@ -440,11 +456,13 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(8)
   const int local = blockIdx.x / splits, r = row0 + local, s = blockIdx.x % splits, tid = threadIdx.x;
   Pieces<kBf16, NV, kScanThreads> z;
   z.load(p, r, s);  // ahead of the settings
-  const Mode mode = row_mode(p, r);
+  const Rules rules = row_rules(p, r);
+  const Mode mode = rules.mode;
   const RowView ws(p, local, splits);
   SplitPart& out = ws.split[s];
   if (s == 0 && tid == 0) {
     ws.row->n_cut = ws.row->n_pick = 0;
+    ws.row->t_cut = -1;
     ws.row->slow = mode == Mode::Slow;
   }
   if (mode == Mode::Slow) return;
@@ -465,10 +483,11 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(8)
     return;
   }
   if (mode == Mode::Full) {
-    const Grid grid{kPerNat / (p.temperature ? static_cast<double>(p.temperature[r]) : 1.0)};
+    const Grid grid{kPerNat / static_cast<double>(rules.tau)};
     const double grid_top = floor(grid.at(top));
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
+      __builtin_amdgcn_sched_barrier(0);  // piece after piece: interleaved they spill 59 registers
 #pragma unroll
       for (int j = 0; j < Pieces<kBf16, NV, kScanThreads>::kPer; ++j) {
         const double g = static_cast<double>(z.logit(i, j)) * grid.scale, b = floor(g);
@@ -482,39 +501,34 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(8)
       }
     }
     __syncthreads();
-    unsigned long long sum = 0;
+    for (int b = tid; b < kGridBins; b += kScanThreads) {
+      unsigned long long sum = 0;
 #pragma unroll
-    for (int c = 0; c < kCopies; ++c) sum += s_bin[tid * kCopies + c];
-    out.data[tid] = sum;
+      for (int c = 0; c < kCopies; ++c) sum += s_bin[b * kCopies + c];
+      out.data[b] = sum;
+    }
     return;
   }
   uint32_t cut = top;
+  int turn = 0;
   if (mode == Mode::TopK) {
     // At least k pieces reach the k-th largest of the pieces' largest logits, so at
     // least k tokens do, and few more while there are many more pieces than k.
-    const int k = p.top_k[r];
-    int turn = 0;
+    const int k = rules.k;
     auto pieces = [&](uint32_t least) {
       int c = 0;
 #pragma unroll
       for (int i = 0; i < NV; ++i) c += popc64(__ballot(most[i] >= least));
-      return block_count(c, s_part, turn++);
+      return block_count<kScanThreads>(c, s_part, turn++);
     };
-    // every thread's largest logit is at least the smallest of them, and k < kScanThreads
+    // every thread's largest logit is at least the smallest of them
     cut = max(low, kKeyNegInf + 1);
-    if (pieces(cut) >= k) cut = bisect<uint32_t>(cut, top, k, k + k / 8 + 8, pieces);
-    auto tokens = [&](uint32_t least) {
-      int c = 0;
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        if (__ballot(most[i] >= least) == 0) continue;
-#pragma unroll
-        for (int j = 0; j < Pieces<kBf16, NV, kScanThreads>::kPer; ++j) c += popc64(__ballot(token_key(z.logit(i, j)) >= least));
-      }
-      return block_count(c, s_part, turn++);
-    };
-    // many tokens per piece reach it only when k is a good part of the pieces
-    if (k > kCandCap / 4 && tokens(cut) > kCandCap) cut = bisect<uint32_t>(cut, top, k, kCandCap, tokens);
+    int c = pieces(cut);
+    if (c < k && cut > kKeyNegInf + 1) {
+      cut = kKeyNegInf + 1;
+      c = pieces(cut);
+    }
+    if (c > k) cut = bisect<uint32_t>(cut, top, k, k + k / 8 + 8, pieces);
   }
   if (mode == Mode::Greedy) {
     // the lowest index of the largest logit
@@ -550,18 +564,35 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(8)
   }
   __syncthreads();
   constexpr int kPer = Pieces<kBf16, NV, kScanThreads>::kPer;
-  const int queued = s_queued;
-  for (int i = tid; i < min(queued, kCandCap) * kPer; i += kScanThreads) {
+  const int queued = s_queued, waiting = min(queued, kCandCap) * kPer;
+  auto queued_key = [&](int i) {
     const int j = i % kPer;
     const uint32_t* w = reinterpret_cast<const uint32_t*>(queue + i / kPer);
-    const uint32_t bits = kBf16 ? (j % 2 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16) : w[j];
-    const uint32_t key = token_key(__uint_as_float(bits));
-    if (key >= cut) {
+    return token_key(__uint_as_float(kBf16 ? (j % 2 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16) : w[j]));
+  };
+  auto list = [&]() {
+    for (int i = tid; i < waiting; i += kScanThreads) {
+      const uint32_t key = queued_key(i);
+      if (key < cut) continue;
       const int at = atomicAdd(&s_n, 1);
-      if (at < kCandCap) out.data[at] = token_order(key, first[i / kPer] + j);
+      if (at < kCandCap) out.data[at] = token_order(key, first[i / kPer] + i % kPer);
     }
+    __syncthreads();
+  };
+  list();
+  if (mode == Mode::TopK && s_n > kCandCap && queued <= kCandCap) {
+    // a top_k of a good part of the pieces: cut by tokens
+    cut = bisect<uint32_t>(cut, top, rules.k, kCandCap, [&](uint32_t least) {
+      int c = 0;
+      for (int i = 0; i < waiting; i += kScanThreads)
+        c += popc64(__ballot(i + tid < waiting && queued_key(i + tid) >= least));
+      return block_count<kScanThreads>(c, s_part, turn++);
+    });
+    __syncthreads();
+    if (tid == 0) s_n = 0;
+    __syncthreads();
+    list();
   }
-  __syncthreads();
   if (tid == 0) {
     out.n = queued > kCandCap ? queued : s_n;
     out.cut = cut;
@@ -620,11 +651,11 @@ __device__ __forceinline__ Sorted sort_and_sum(unsigned long long v, int n, unsi
 }
 
 struct PickShared {
-  unsigned long long fine[kScanThreads];
-  unsigned long long buf[kScanThreads];
-  double part[kScanThreads / kWave];
+  unsigned long long fine[kBlockThreads];
+  unsigned long long buf[kBlockThreads];
+  double part[kBlockThreads / kWave];
   double value;
-  int part32[2 * kScanThreads / kWave];
+  int part32[2 * kBlockThreads / kWave];
   int offset[kMaxSplits + 1];  // candidates in front of each split's
   int n, at;
 };
@@ -655,12 +686,17 @@ __device__ __forceinline__ unsigned long long candidate(const RowView& ws, const
   return ws.split[s].data[i - offset[s]];
 }
 
-// The cut that leaves exactly k of the candidates; at least k have a key >= least.
+// The cut that leaves exactly k of the candidates; at least k have a key >= least.  Keys of
+// bf16 logits differ in their upper half only (below it zeros, or ones if negative).  Empty
+// places are 0, which no mid reaches.
 template <class CountKeys, class CountTokens>
-__device__ __forceinline__ unsigned long long cut_to(int k, uint32_t least, uint32_t top, CountKeys keys,
-                                                     CountTokens tokens) {
-  const uint32_t key = bisect<uint32_t>(least, top, k, k, keys);
-  return bisect<unsigned long long>(static_cast<unsigned long long>(key) << 32, token_order(key, 0), k, k, tokens);
+__device__ __forceinline__ unsigned long long cut_to(const SampleParams& p, int k, uint32_t least, uint32_t top,
+                                                     CountKeys keys, CountTokens tokens) {
+  const int shift = p.is_bf16 ? 16 : 0;
+  uint32_t key = bisect<uint32_t>(least >> shift, top >> shift, k, k, [&](uint32_t m) { return keys(m << shift); })
+                 << shift;
+  if (p.is_bf16 && !(key & 0x80000000u)) key |= 0xffffu;
+  return bisect<unsigned long long>(token_order(key, p.V - 1), token_order(key, 0), k, k, tokens);
 }
 
 // Up to 64 EL candidates left: one wave orders them, value e of a lane at place 64 e + lane.
@@ -716,10 +752,10 @@ __device__ __forceinline__ double wave_value(const double (&v)[EL], int place) {
 }
 
 template <int EL>
-__device__ void wave_pick(const SampleParams& p, int r, uint32_t top, int k, unsigned long long (&v)[EL]) {
+__device__ void wave_pick(const SampleParams& p, int r, const Rules& rules, uint32_t top, int k, unsigned long long (&v)[EL]) {
   const int lane = lane_id();
   wave_sort(v);
-  const RowRule rule{top, key_logit(top), p.temperature ? p.temperature[r] : 1.f};
+  const RowRule rule{top, key_logit(top), rules.tau};
   double w[EL], sum[EL], before = 0.0;
 #pragma unroll
   for (int e = 0; e < EL; ++e) {
@@ -734,21 +770,21 @@ __device__ void wave_pick(const SampleParams& p, int r, uint32_t top, int k, uns
   }
   bool hit[EL];
   int keep = k;
-  if (p.top_p && !(p.top_p[r] >= 1.f)) {
-    const double want = fmax(static_cast<double>(p.top_p[r]), 0.0) * before;
+  if (rules.by_p()) {
+    const double want = rules.top_p * before;
 #pragma unroll
     for (int e = 0; e < EL; ++e) hit[e] = sum[e] >= want;
     keep = min(keep, wave_first(hit) + 1);
   }
-  if (p.min_p && p.min_p[r] > 0.f) {
-    const double m = fmin(static_cast<double>(p.min_p[r]), 1.0);
+  if (rules.by_m()) {
+    const double m = rules.min_p;
 #pragma unroll
     for (int e = 0; e < EL; ++e) hit[e] = w[e] < m;
     keep = min(keep, wave_first(hit));
   }
   keep = max(keep, 1);
   const double total = wave_value(sum, keep - 1);
-  const double at = row_uniform(p, r) * total;
+  const double at = rules.u * total;
 #pragma unroll
   for (int e = 0; e < EL; ++e) hit[e] = sum[e] > at;
   const int j = min(wave_first(hit), keep - 1);
@@ -766,9 +802,9 @@ enum class Picked { Done, Block, Slow };
 
 // Candidates of a greedy or top-k row -> token.  Up to 1024 candidates and a top_k of 256
 // the first wave does it all in registers (a workgroup with its barriers took 18 us
-// instead); more are for a workgroup of kScanThreads (kBlock).
+// instead); more are for a workgroup of kBlockThreads (kBlock).
 template <bool kBlock, class Shared>
-__device__ Picked pick_candidates(const SampleParams& p, int r, Mode mode, const RowView& ws, int splits, Shared& sh) {
+__device__ Picked pick_candidates(const SampleParams& p, int r, const Rules& rules, const RowView& ws, int splits, Shared& sh) {
   const int tid = threadIdx.x, lane = lane_id();
   // every wave reads the splits' heads, one per lane
   const int ns = lane < splits ? ws.split[lane].n : 0;
@@ -781,7 +817,7 @@ __device__ Picked pick_candidates(const SampleParams& p, int r, Mode mode, const
     if (tid == 0) p.token[r] = -1, p.prob[r] = 0.f;
     return Picked::Done;
   }
-  if (mode == Mode::Greedy) {
+  if (rules.mode == Mode::Greedy) {
     if (tid < kWave) {
       unsigned long long best = ns > 0 ? ws.split[lane].data[0] : 0;
       for (int o = 32; o >= 1; o >>= 1) best = max(best, __shfl_xor(best, o));
@@ -789,7 +825,7 @@ __device__ Picked pick_candidates(const SampleParams& p, int r, Mode mode, const
     }
     return Picked::Done;
   }
-  const int k = min(p.top_k[r], n);
+  const int k = min(rules.k, n);
   // a split with k candidates of its own: at least k of the row reach its cut
   uint32_t least = lane < splits && ns >= k ? ws.split[lane].cut : 0;
   for (int o = 32; o >= 1; o >>= 1) least = max(least, static_cast<uint32_t>(__shfl_xor(least, o)));
@@ -805,19 +841,19 @@ __device__ Picked pick_candidates(const SampleParams& p, int r, Mode mode, const
 #pragma unroll
     for (int i = 0; i < kWaveMine; ++i) mine[i] = lane + i * kWave < n ? candidate(ws, sh.offset, lane + i * kWave) : 0;
     const unsigned long long cut = cut_to(
-        k, least, top,
+        p, k, least, top,
         [&](uint32_t key) {
           int c = 0;
 #pragma unroll
           for (int i = 0; i < kWaveMine; ++i)
-            if (i * kWave < n) c += popc64(__ballot(order_key(mine[i]) >= key && mine[i] != 0));
+            if (i * kWave < n) c += popc64(__ballot(order_key(mine[i]) >= key));
           return c;
         },
         [&](unsigned long long token) {
           int c = 0;
 #pragma unroll
           for (int i = 0; i < kWaveMine; ++i)
-            if (i * kWave < n) c += popc64(__ballot(mine[i] >= token && mine[i] != 0));
+            if (i * kWave < n) c += popc64(__ballot(mine[i] >= token));
           return c;
         });
     int at = 0;
@@ -831,16 +867,16 @@ __device__ Picked pick_candidates(const SampleParams& p, int r, Mode mode, const
     wave_lds_sync();
     if (k <= kWave) {
       unsigned long long v[1] = {lane < k ? sh.buf[lane] : 0};
-      wave_pick<1>(p, r, top, k, v);
+      wave_pick<1>(p, r, rules, top, k, v);
     } else {
       unsigned long long v[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = e * kWave + lane < k ? sh.buf[e * kWave + lane] : 0;
       if (k <= 2 * kWave) {
         unsigned long long h[2] = {v[0], v[1]};
-        wave_pick<2>(p, r, top, k, h);
+        wave_pick<2>(p, r, rules, top, k, h);
       } else {
-        wave_pick<4>(p, r, top, k, v);
+        wave_pick<4>(p, r, rules, top, k, v);
       }
     }
     return Picked::Done;
@@ -849,27 +885,27 @@ __device__ Picked pick_candidates(const SampleParams& p, int r, Mode mode, const
     return Picked::Block;
   } else {
     __syncthreads();
-    constexpr int kMine = kCandMax / kScanThreads;
+    constexpr int kMine = kCandMax / kBlockThreads;
     unsigned long long mine[kMine];
 #pragma unroll
     for (int i = 0; i < kMine; ++i)
-      mine[i] = tid + i * kScanThreads < n ? candidate(ws, sh.offset, tid + i * kScanThreads) : 0;
+      mine[i] = tid + i * kBlockThreads < n ? candidate(ws, sh.offset, tid + i * kBlockThreads) : 0;
     int turn = 0;
     const unsigned long long cut = cut_to(
-        k, least, top,
+        p, k, least, top,
         [&](uint32_t key) {
           int c = 0;
 #pragma unroll
           for (int i = 0; i < kMine; ++i)
-            if (i * kScanThreads < n) c += popc64(__ballot(order_key(mine[i]) >= key && mine[i] != 0));
-          return block_count(c, sh.part32, turn++);
+            if (i * kBlockThreads < n) c += popc64(__ballot(order_key(mine[i]) >= key));
+          return block_count<kBlockThreads>(c, sh.part32, turn++);
         },
         [&](unsigned long long token) {
           int c = 0;
 #pragma unroll
           for (int i = 0; i < kMine; ++i)
-            if (i * kScanThreads < n) c += popc64(__ballot(mine[i] >= token && mine[i] != 0));
-          return block_count(c, sh.part32, turn++);
+            if (i * kBlockThreads < n) c += popc64(__ballot(mine[i] >= token));
+          return block_count<kBlockThreads>(c, sh.part32, turn++);
         });
     __syncthreads();
     if (tid == 0) sh.n = 0;
@@ -879,18 +915,18 @@ __device__ Picked pick_candidates(const SampleParams& p, int r, Mode mode, const
       if (mine[i] >= cut && mine[i] != 0) sh.buf[atomicAdd(&sh.n, 1)] = mine[i];  // k in all
     __syncthreads();
     const unsigned long long v = tid < k ? sh.buf[tid] : 0;
-    const RowRule rule{top, key_logit(top), p.temperature ? p.temperature[r] : 1.f};
+    const RowRule rule{top, key_logit(top), rules.tau};
     const Sorted t = sort_and_sum(v, k, sh.buf, sh.part, [&](uint32_t key) { return rule.weight(key); });
     int keep = k;
-    if (p.top_p && !(p.top_p[r] >= 1.f)) {
-      const double want = fmax(static_cast<double>(p.top_p[r]), 0.0) * thread_value(t.sum, k - 1, sh);
+    if (rules.by_p()) {
+      const double want = rules.top_p * thread_value(t.sum, k - 1, sh);
       keep = min(keep, first_thread(tid < k && t.sum >= want, k, sh) + 1);
     }
-    if (p.min_p && p.min_p[r] > 0.f)
-      keep = min(keep, first_thread(tid >= k || t.weight < fmin(static_cast<double>(p.min_p[r]), 1.0), k, sh));
+    if (rules.by_m())
+      keep = min(keep, first_thread(tid >= k || t.weight < rules.min_p, k, sh));
     keep = max(keep, 1);
     const double total = thread_value(t.sum, keep - 1, sh);
-    const double at = row_uniform(p, r) * total;
+    const double at = rules.u * total;
     if (tid == first_thread(tid < keep && t.sum > at, keep - 1, sh)) {
       p.token[r] = order_index(t.token);
       p.prob[r] = static_cast<float>(t.weight / total);
@@ -933,32 +969,26 @@ __device__ __forceinline__ double bin_value(const double (&v)[kFilterMine], int 
   return sh.value;
 }
 
-// Workgroup b takes row b % rows, part b / rows: the parts that do a whole top-k row come
-// first and go to all XCDs in turn (workgroup b runs on XCD b % 8; with a row's parts side
-// by side they fell on two of them, 132 us of 512 x 100003).
-template <bool kBf16, int NV>
-__global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SampleParams p, int row0, int rows, int splits) {
+// One workgroup per row: a greedy or top-k row's token from its candidates, else the bins in
+// which the kept prefix ends and in which the sample lies.
+__global__ __launch_bounds__(kFilterThreads) void sample_place_kernel(SampleParams p, int row0, int splits) {
   __shared__ FilterShared sh;
-  const int local = blockIdx.x % rows, r = row0 + local, s = blockIdx.x / rows, tid = threadIdx.x;
-  const Mode mode = row_mode(p, r);
+  const int local = blockIdx.x, r = row0 + local, tid = threadIdx.x;
   const RowView ws(p, local, splits);
-  if (mode == Mode::Slow) return;
-  if (mode != Mode::Full) {
-    if (s != 0) return;
-    const Picked done = pick_candidates<false>(p, r, mode, ws, splits, sh);
+  const Rules rules = row_rules(p, r);
+  if (rules.mode == Mode::Slow) return;
+  if (rules.mode != Mode::Full) {
+    const Picked done = pick_candidates<false>(p, r, rules, ws, splits, sh);
     if (tid == 0 && done != Picked::Done) ws.row->slow = done == Picked::Slow ? 1 : 2;
     return;
   }
-  Pieces<kBf16, NV, kFilterThreads> z;
-  z.load(p, r, s);  // needed last, requested first
   uint32_t top = lane_id() < splits ? ws.split[lane_id()].top : 0;
   for (int o = 32; o >= 1; o >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(top, o)));
-  const double tau = p.temperature ? static_cast<double>(p.temperature[r]) : 1.0;
-  const Grid grid{kPerNat / tau};
+  const Grid grid{kPerNat / static_cast<double>(rules.tau)};
   const double grid_top = floor(grid.at(top));
   // far from 0 the grid's 64 bits no longer hold the weights' digits
   const bool slow = !(fabs(grid.at(top)) < 33554432.0);
-  if (s == 0 && tid == 0) {
+  if (tid == 0) {
     ws.row->top = top;
     ws.row->slow = slow && top > kKeyNegInf;
     ws.row->grid_top = grid_top;
@@ -1002,41 +1032,47 @@ __global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SamplePar
   };
   int cut = -1;
   double kept = total, least = total;  // the kept sum lies between
-  if (p.top_p && !(p.top_p[r] >= 1.f)) {
-    const double want = fmax(static_cast<double>(p.top_p[r]), 0.0) * total;
+  if (rules.by_p()) {
+    const double want = rules.top_p * total;
     cut = first([&](double v) { return v >= want; }, kGridBins - 1);
   }
-  if (p.min_p && p.min_p[r] > 0.f) {
-    const double m = fmin(static_cast<double>(p.min_p[r]), 1.0);
-    const double t = grid_top - floor(grid.at(top) + kPerNat * log(m));
+  if (rules.by_m()) {
+    const double t = grid_top - floor(grid.at(top) + kPerNat * log(rules.min_p));
     if (t < (cut < 0 ? kGridBins : cut)) cut = static_cast<int>(t);
   }
   if (cut >= 0) {
     kept = bin_value(incl, cut, sh);
     least = bin_value(excl, cut, sh);
   }
-  const double u = row_uniform(p, r);
   // the last bin that holds a kept weight, for roundings at the end
   const int last = cut >= 0 ? cut : first([&](double v) { return v >= total; }, kGridBins - 1);
-  const int pick0 = first([&](double v) { return v > u * least; }, last);
-  const int pick1 = kept > least ? first([&](double v) { return v > u * kept; }, last) : pick0;
-  if (s == 0) {
+  const int pick0 = first([&](double v) { return v > rules.u * least; }, last);
+  const int pick1 = kept > least ? first([&](double v) { return v > rules.u * kept; }, last) : pick0;
 #pragma unroll
-    for (int e = 0; e < kFilterMine; ++e) {
-      if (tid * kFilterMine + e == pick0) ws.row->before_pick = excl[e];
-      if (tid * kFilterMine + e == cut) ws.row->before_cut = excl[e];
-    }
-    if (tid == 0) {
-      ws.row->t_cut = cut;
-      ws.row->t_pick0 = pick0;
-      ws.row->t_pick1 = pick1;
-      ws.row->total = total;
-    }
+  for (int e = 0; e < kFilterMine; ++e) {
+    if (tid * kFilterMine + e == pick0) ws.row->before_pick = excl[e];
+    if (tid * kFilterMine + e == cut) ws.row->before_cut = excl[e];
   }
-  // which of this thread's tokens lie in those bins (32 tokens at most), then room for
-  // them: one counter per list in LDS, one addition to the row's per workgroup
-  constexpr int kPer = Pieces<kBf16, NV, kFilterThreads>::kPer;
+  if (tid == 0) {
+    ws.row->t_cut = cut;
+    ws.row->t_pick0 = pick0;
+    ws.row->t_pick1 = pick1;
+    ws.row->total = total;
+  }
+}
+
+struct FilterCounts {
+  int n_cut, n_pick, cut0, pick0;
+};
+
+// Lists the tokens of part s of a row that lie in the named bins: a bit per token of this
+// thread, then one counter per list in LDS and one addition to the row's per workgroup.
+template <bool kBf16, int NV, int kThreads>
+__device__ __forceinline__ void list_tokens(const Pieces<kBf16, NV, kThreads>& z, const Grid& grid, RowPart& row,
+                                            FilterCounts& sh) {
+  constexpr int kPer = Pieces<kBf16, NV, kThreads>::kPer;
   static_assert(NV * kPer <= 32, "a bit per token");
+  const double grid_top = row.grid_top, cut = row.t_cut, pick0 = row.t_pick0, pick1 = row.t_pick1;
   uint32_t in_cut = 0, in_pick = 0;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -1047,14 +1083,14 @@ __global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SamplePar
       in_pick |= t >= pick0 && t <= pick1 ? 1u << (i * kPer + j) : 0u;
     }
   }
-  if (tid == 0) sh.n_cut = sh.n_pick = 0;
+  if (threadIdx.x == 0) sh.n_cut = sh.n_pick = 0;
   __syncthreads();
   int at_cut = in_cut ? atomicAdd(&sh.n_cut, __popc(in_cut)) : 0;
   int at_pick = in_pick ? atomicAdd(&sh.n_pick, __popc(in_pick)) : 0;
   __syncthreads();
-  if (tid == 0) {
-    sh.cut0 = sh.n_cut ? atomicAdd(&ws.row->n_cut, sh.n_cut) : 0;
-    sh.pick0 = sh.n_pick ? atomicAdd(&ws.row->n_pick, sh.n_pick) : 0;
+  if (threadIdx.x == 0) {
+    sh.cut0 = sh.n_cut ? atomicAdd(&row.n_cut, sh.n_cut) : 0;
+    sh.pick0 = sh.n_pick ? atomicAdd(&row.n_pick, sh.n_pick) : 0;
   }
   __syncthreads();
   at_cut += sh.cut0;
@@ -1067,15 +1103,27 @@ __global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SamplePar
       if (((in_cut | in_pick) & bit) == 0) continue;
       const unsigned long long token = token_order(token_key(z.logit(i, j)), z.index(i, j));
       if (in_cut & bit) {
-        if (at_cut < kListCap) ws.row->cut[at_cut] = token;
+        if (at_cut < kListCap) row.cut[at_cut] = token;
         ++at_cut;
       }
       if (in_pick & bit) {
-        if (at_pick < kListCap) ws.row->pick[at_pick] = token;
+        if (at_pick < kListCap) row.pick[at_pick] = token;
         ++at_pick;
       }
     }
   }
+}
+
+template <bool kBf16, int NV>
+__global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SampleParams p, int row0, int rows, int splits) {
+  __shared__ FilterCounts sh;
+  const int local = blockIdx.x % rows, r = row0 + local, s = blockIdx.x / rows;
+  Pieces<kBf16, NV, kFilterThreads> z;
+  z.load(p, r, s);
+  const RowView ws(p, local, splits);
+  const Rules rules = row_rules(p, r);
+  if (rules.mode != Mode::Full || ws.row->slow || ws.row->top <= kKeyNegInf) return;
+  list_tokens(z, Grid{kPerNat / static_cast<double>(rules.tau)}, *ws.row, sh);
 }
 
 union FinishShared {
@@ -1083,23 +1131,39 @@ union FinishShared {
   PickShared pick;
 };
 
-// A listed range of bins in a workgroup's registers: token and weight, in 2^-43 of the
-// range's first bin (whole numbers: sums in any order are the same).
+__device__ __forceinline__ unsigned long long wave_sum_u64(unsigned long long v) {
+  auto add = [](double a, double b) {
+    return __longlong_as_double(__double_as_longlong(a) + __double_as_longlong(b));
+  };
+  return static_cast<unsigned long long>(__double_as_longlong(dpp::reduce(__longlong_as_double(v), 0.0, add)));
+}
+
+// A listed range of bins in the registers of a wave (up to 1024 tokens) or a workgroup of
+// kBlockThreads: token and weight, in 2^-43 of the range's first bin (whole numbers: sums in
+// any order are the same).
+template <bool kBlock>
 struct Listed {
-  static constexpr int kMine = kListCap / kScanThreads;
+  static constexpr int kThreads = kBlock ? kBlockThreads : kWave;
+  static constexpr int kMine = kBlock ? kListCap / kBlockThreads : kWaveList / kWave;
   unsigned long long token[kMine], weight[kMine];
   double unit;  // what 1 of them stands for
+  int n;
 
-  __device__ __forceinline__ Listed(const unsigned long long* list, int n, const Grid& grid, double grid_top, int t0)
-      : unit(exp(-t0 / kPerNat) / kWeightOne) {
+  __device__ __forceinline__ Listed(const unsigned long long* list, int n_) : n(n_) {
+    const int me = kBlock ? static_cast<int>(threadIdx.x) : lane_id();
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) token[i] = me + i * kThreads < n ? list[me + i * kThreads] : 0;
+  }
+  __device__ __forceinline__ void weigh(const Grid& grid, double grid_top, int t0) {
+    unit = exp(-t0 / kPerNat) / kWeightOne;
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
-      token[i] = weight[i] = 0;
-      const int at = static_cast<int>(threadIdx.x) + i * kScanThreads;
-      if (at >= n) continue;
-      token[i] = list[at];
-      const double g = grid.at(order_key(token[i])), b = floor(g);
-      weight[i] = __double2ull_rn(Grid::weight(g - b) * exp((b + t0 - grid_top) / kPerNat) * kWeightOne);
+      weight[i] = 0;
+      if (i * kThreads >= n) continue;
+      const double g = grid.at(order_key(token[i])), b = floor(g), below = grid_top - t0 - b;
+      double w = Grid::weight(g - b);
+      if (__ballot(token[i] != 0 && below != 0.0) != 0) w *= exp(-below / kPerNat);  // mostly the list is one bin
+      weight[i] = token[i] != 0 ? __double2ull_rn(w * kWeightOne) : 0;
     }
   }
 };
@@ -1109,66 +1173,72 @@ struct Sums {
   int count;
 };
 
-// Workgroup-wide sums; one barrier a call, calls in a row alternate between two halves.
-__device__ __forceinline__ Sums block_sums(unsigned long long w, int c, PickShared& sh, int turn) {
-  constexpr int kWaves = kScanThreads / kWave;
-  for (int o = 32; o >= 1; o >>= 1) w += __shfl_xor(w, o);
-  if (lane_id() == 0) {
-    sh.fine[(turn & 1) * kWaves + wave_id()] = w;
-    sh.part32[(turn & 1) * kWaves + wave_id()] = c;
+// Sums over the wave, or the workgroup: there one barrier a call, calls in a row alternate
+// between two halves of the shared words.
+template <bool kBlock>
+__device__ __forceinline__ Sums group_sums(unsigned long long w, int c, PickShared& sh, int turn) {
+  w = wave_sum_u64(w);
+  if constexpr (!kBlock) {
+    return {w, c};
+  } else {
+    constexpr int kWaves = kBlockThreads / kWave;
+    const int half = (turn & 1) * kWaves;
+    if (lane_id() == 0) {
+      sh.fine[half + wave_id()] = w;
+      sh.part32[half + wave_id()] = c;
+    }
+    __syncthreads();
+    const int at = half + lane_id() % kWaves;
+    return {wave_sum_u64(lane_id() < kWaves ? sh.fine[at] : 0), wave_sum_i32(lane_id() < kWaves ? sh.part32[at] : 0)};
   }
-  __syncthreads();
-  unsigned long long v = sh.fine[(turn & 1) * kWaves + lane_id() % kWaves];
-  for (int o = kWaves / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o);
-  return {v, wave_sum_i32(sh.part32[(turn & 1) * kWaves + lane_id() % kWaves]) / (kWave / kWaves)};
+}
+
+template <bool kBlock>
+__device__ __forceinline__ void group_sync() {
+  if constexpr (kBlock) __syncthreads();
+  else wave_lds_sync();
 }
 
 // The token of a list at which passes(before + sum up to it) turns true, and that sum; the
 // list's last one if it never does.  The order is searched by halves until at most 64 tokens
-// are left around the place, and those are sorted by every wave for itself.
+// are left around the place, and those are sorted.
 struct PlaceInList {
   unsigned long long token;
   double sum;
 };
-template <class Passes>
-__device__ __forceinline__ PlaceInList place_in_list(const Listed& l, int n, double before, PickShared& sh, Passes passes) {
-  unsigned long long lo = 1, hi = ~0ull;  // tokens in [lo, hi): the place and its neighbours
-  Sums above = {0, 0};                    // of tokens from hi on
-  int inside = n, turn = 0;
-  // every token lies in [least, most]: a list's keys share their upper bits
-  unsigned long long least = ~0ull, most = 0;
+template <bool kBlock, class Passes>
+__device__ __forceinline__ PlaceInList place_in_list(const Listed<kBlock>& l, double before, PickShared& sh,
+                                                     Passes passes) {
+  const int lane = lane_id();
+  // every token lies in [lo, hi): a list's keys share their upper bits
+  uint32_t least = ~0u, most = 0;
 #pragma unroll
-  for (int i = 0; i < Listed::kMine; ++i) {
-    if (l.token[i] == 0) continue;
-    least = min(least, l.token[i]);
-    most = max(most, l.token[i]);
+  for (int i = 0; i < Listed<kBlock>::kMine; ++i) {
+    least = min(least, l.token[i] != 0 ? order_key(l.token[i]) : ~0u);
+    most = max(most, order_key(l.token[i]));
   }
-  for (int o = 32; o >= 1; o >>= 1) {
-    least = min(least, __shfl_xor(least, o));
-    most = max(most, __shfl_xor(most, o));
+  if constexpr (kBlock) {
+    block_range(most, least, reinterpret_cast<uint32_t*>(sh.buf));
+  } else {
+    auto larger = [](uint32_t a, uint32_t b) { return max(a, b); };
+    most = dpp::reduce(most, 0u, larger);
+    least = ~dpp::reduce(~least, 0u, larger);
   }
-  __syncthreads();
-  if (lane_id() == 0) {
-    sh.buf[wave_id()] = least;
-    sh.buf[kScanThreads / kWave + wave_id()] = most;
-  }
-  __syncthreads();
-  for (int w = 0; w < kScanThreads / kWave; ++w) {
-    least = min(least, sh.buf[w]);
-    most = max(most, sh.buf[kScanThreads / kWave + w]);
-  }
-  lo = least;
-  hi = most + 1;
+  unsigned long long lo = static_cast<unsigned long long>(least) << 32;
+  unsigned long long hi = (static_cast<unsigned long long>(most) + 1) << 32;
+  Sums above = {0, 0};  // of tokens from hi on
+  int inside = l.n, turn = 0;
   while (inside > kWave && hi - lo > 1) {
     const unsigned long long mid = lo + (hi - lo) / 2;
     unsigned long long w = 0;
     int c = 0;
 #pragma unroll
-    for (int i = 0; i < Listed::kMine; ++i) {
+    for (int i = 0; i < Listed<kBlock>::kMine; ++i) {
+      if (i * Listed<kBlock>::kThreads >= l.n) continue;
       w += l.token[i] >= mid ? l.weight[i] : 0;
       c += popc64(__ballot(l.token[i] >= mid));
     }
-    const Sums s = block_sums(w, c, sh, turn++);
+    const Sums s = group_sums<kBlock>(w, c, sh, turn++);
     if (passes(before + static_cast<double>(s.weight) * l.unit)) {
       lo = mid;
       inside = s.count - above.count;
@@ -1178,19 +1248,20 @@ __device__ __forceinline__ PlaceInList place_in_list(const Listed& l, int n, dou
       above = s;
     }
   }
-  __syncthreads();
+  group_sync<kBlock>();
   if (threadIdx.x == 0) sh.n = 0;
-  __syncthreads();
+  group_sync<kBlock>();
 #pragma unroll
-  for (int i = 0; i < Listed::kMine; ++i) {
-    if (l.token[i] < lo || l.token[i] >= hi) continue;
+  for (int i = 0; i < Listed<kBlock>::kMine; ++i) {
+    if (l.token[i] == 0 || l.token[i] < lo || l.token[i] >= hi) continue;
     const int at = atomicAdd(&sh.n, 1);  // 64 at most
     sh.buf[at] = l.token[i];
     sh.fine[at] = l.weight[i];
   }
-  __syncthreads();
-  const int lane = lane_id(), m = sh.n;
+  group_sync<kBlock>();
+  const int m = sh.n;
   unsigned long long v = lane < m ? sh.buf[lane] : 0, w = lane < m ? sh.fine[lane] : 0;
+  group_sync<kBlock>();
 #pragma unroll
   for (int run = 2; run <= kWave; run *= 2) {
 #pragma unroll
@@ -1211,65 +1282,97 @@ __device__ __forceinline__ PlaceInList place_in_list(const Listed& l, int n, dou
   return {__shfl(v, at), __shfl(sum, at)};
 }
 
-template <bool kBf16>
-__global__ __launch_bounds__(kRowThreads) void sample_finish_kernel(SampleParams p, int row0, int splits) {
-  __shared__ FinishShared un;
-  const int local = blockIdx.x, r = row0 + local, tid = threadIdx.x;
-  const RowView ws(p, local, splits);
-  const RowPart& in = *ws.row;
-  if (in.slow == 2) {
-    pick_candidates<true>(p, r, Mode::TopK, ws, splits, un.pick);
-    return;
-  }
-  if (in.slow) {
-    sample_row<kBf16>(p, r, un.row);
-    return;
-  }
-  if (row_mode(p, r) != Mode::Full) return;
-  const uint32_t top = in.top;
-  if (top <= kKeyNegInf) {
-    if (tid == 0) p.token[r] = -1, p.prob[r] = 0.f;
-    return;
-  }
-  const int n_cut = in.t_cut >= 0 ? in.n_cut : 0, n_pick = in.n_pick;
-  if (n_cut > kListCap || n_pick > kListCap) {
-    sample_row<kBf16>(p, r, un.row);
-    return;
-  }
-  PickShared& sh = un.pick;
-  const double tau = p.temperature ? static_cast<double>(p.temperature[r]) : 1.0;
-  const Grid grid{kPerNat / tau};
-  const double grid_top = in.grid_top;
-  double total = in.total;
-  if (in.t_cut >= 0) {
+// The token of a row whose bins are listed, by one wave or the workgroup.
+template <bool kBlock>
+__device__ void finish_row(const SampleParams& p, int r, const Rules& rules, const RowPart& in, const RowHead& head,
+                           int n_cut, int n_pick, PickShared& sh) {
+  const Grid grid{kPerNat / static_cast<double>(rules.tau)};
+  const double grid_top = head.grid_top;
+  double total = head.total;
+  if (head.t_cut >= 0) {
     // both filters keep a prefix: the shorter one
-    const Listed l(in.cut, n_cut, grid, grid_top, in.t_cut);
+    Listed<kBlock> l(in.cut, n_cut);
+    l.weigh(grid, grid_top, head.t_cut);
     double kept = INFINITY;
-    if (p.top_p && !(p.top_p[r] >= 1.f)) {
-      const double want = fmax(static_cast<double>(p.top_p[r]), 0.0) * total;
-      const PlaceInList at = place_in_list(l, n_cut, in.before_cut, sh, [&](double sum) { return sum >= want; });
+    if (rules.by_p()) {
+      const double want = rules.top_p * total;
+      const PlaceInList at = place_in_list(l, head.before_cut, sh, [&](double sum) { return sum >= want; });
       if (at.sum >= want) kept = at.sum;
     }
-    if (p.min_p && p.min_p[r] > 0.f) {
-      const RowRule rule{top, key_logit(top), tau};
-      const double m = fmin(static_cast<double>(p.min_p[r]), 1.0);
+    if (rules.by_m()) {
+      const RowRule rule{head.top, key_logit(head.top), rules.tau};
+      const double m = rules.min_p;
       unsigned long long w = 0;
 #pragma unroll
-      for (int i = 0; i < Listed::kMine; ++i)
+      for (int i = 0; i < Listed<kBlock>::kMine; ++i)
         if (l.token[i] != 0 && rule.weight(order_key(l.token[i])) >= m) w += l.weight[i];
-      __syncthreads();
-      kept = fmin(kept, in.before_cut + static_cast<double>(block_sums(w, 0, sh, 0).weight) * l.unit);
+      group_sync<kBlock>();
+      kept = fmin(kept, head.before_cut + static_cast<double>(group_sums<kBlock>(w, 0, sh, 0).weight) * l.unit);
+      group_sync<kBlock>();
     }
     total = fmin(kept, total);
   }
-  const double at = row_uniform(p, r) * total;
-  const Listed l(in.pick, n_pick, grid, grid_top, in.t_pick0);
-  const PlaceInList j = place_in_list(l, n_pick, in.before_pick, sh, [&](double sum) { return sum > at; });
-  if (tid == 0) {
+  const double at = rules.u * total;
+  Listed<kBlock> l(in.pick, n_pick);
+  l.weigh(grid, grid_top, head.t_pick0);
+  const PlaceInList j = place_in_list(l, head.before_pick, sh, [&](double sum) { return sum > at; });
+  if (threadIdx.x == 0) {
     const double g = grid.at(order_key(j.token)), b = floor(g);
     p.token[r] = order_index(j.token);
     p.prob[r] = static_cast<float>(Grid::weight(g - b) * exp((b - grid_top) / kPerNat) / total);
   }
+}
+
+// A row that is not done yet, by a workgroup.  kList: lists the bins' tokens itself, part after
+// part; used beside top_k, where few rows need it.
+template <bool kBf16, int NV, bool kList>
+__device__ __forceinline__ void finish_one(const SampleParams& p, int row0, int local, int splits, FinishShared& un,
+                                           FilterCounts& counts) {
+  const int r = row0 + local, tid = threadIdx.x;
+  const RowView ws(p, local, splits);
+  RowPart& in = *ws.row;
+  const RowHead head = in;
+  const Rules rules = row_rules(p, r);
+  if (head.slow == 2) {
+    pick_candidates<true>(p, r, rules, ws, splits, un.pick);
+    return;
+  }
+  if (head.slow == 0) {
+    if (rules.mode != Mode::Full) return;
+    if (head.top <= kKeyNegInf) {
+      if (tid == 0) p.token[r] = -1, p.prob[r] = 0.f;
+      return;
+    }
+    int n_cut = head.n_cut, n_pick = head.n_pick;
+    if constexpr (kList) {
+      const Grid grid{kPerNat / static_cast<double>(rules.tau)};
+      for (int s = 0; s * kBlockThreads < splits * kScanThreads; ++s) {
+        Pieces<kBf16, NV, kBlockThreads> z;
+        z.load(p, r, s);
+        __syncthreads();
+        list_tokens(z, grid, in, counts);
+      }
+      __syncthreads();
+      n_cut = __hip_atomic_load(&in.n_cut, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      n_pick = __hip_atomic_load(&in.n_pick, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (n_cut <= kWaveList && n_pick <= kWaveList) {
+      if (wave_id() == 0) finish_row<false>(p, r, rules, in, head, n_cut, n_pick, un.pick);
+      return;
+    }
+    if (n_cut <= kListCap && n_pick <= kListCap) {
+      finish_row<true>(p, r, rules, in, head, n_cut, n_pick, un.pick);
+      return;
+    }
+  }
+  sample_row<kBf16>(p, r, rules, un.row);
+}
+
+template <bool kBf16, int NV, bool kList>
+__global__ __launch_bounds__(kRowThreads) void sample_finish_kernel(SampleParams p, int row0, int splits) {
+  __shared__ FinishShared un;
+  __shared__ FilterCounts counts;
+  finish_one<kBf16, NV, kList>(p, row0, blockIdx.x, splits, un, counts);
 }
 
 // 16-byte pieces per thread: 32 tokens' worth, or fewer while that spreads a row over more
@@ -1277,13 +1380,21 @@ __global__ __launch_bounds__(kRowThreads) void sample_finish_kernel(SampleParams
 struct Shape {
   int nv, splits;
 };
-Shape sample_shape(int R, int V, int is_bf16) {
+Shape sample_shape(int R, int V, int is_bf16, int skew) {
   const int per = is_bf16 ? 8 : 4;
-  const int pieces = (V + 2 * per - 2) / per;  // wherever the row starts
+  const int pieces = (skew + V + per - 1) / per;
   auto splits = [&](int nv) { return (pieces + kScanThreads * nv - 1) / (kScanThreads * nv); };
   int nv = 32 / per;
-  while (nv > 1 && splits(nv / 2) > splits(nv) && splits(nv / 2) <= 16 && R * splits(nv / 2) <= 512) nv /= 2;
+  while (nv > 1 && splits(nv / 2) > splits(nv) && splits(nv / 2) <= 8 && R * splits(nv / 2) <= 1024) nv /= 2;
   return {nv, splits(nv)};
+}
+
+// the most tokens by which a row starts behind a 16-byte boundary
+int row_skew(const SampleParams& p) {
+  const size_t eb = p.is_bf16 ? 2 : 4;
+  const size_t base = reinterpret_cast<uintptr_t>(p.logits) % 16;
+  if (p.R == 1 || p.row_stride * eb % 16 == 0) return static_cast<int>(base / eb);
+  return static_cast<int>(16 / eb) - 1;
 }
 
 template <bool kBf16, int NV>
@@ -1291,9 +1402,14 @@ hipError_t launch_sample_nv(const SampleParams& p, int splits, hipStream_t strea
   for (int row0 = 0; row0 < p.R; row0 += kRowsPerLaunch) {
     const int rows = p.R - row0 < kRowsPerLaunch ? p.R - row0 : kRowsPerLaunch;
     sample_scan_kernel<kBf16, NV><<<rows * splits, kScanThreads, 0, stream>>>(p, row0, splits);
-    sample_filter_kernel<kBf16, NV><<<rows * splits * (kScanThreads / kFilterThreads), kFilterThreads, 0, stream>>>(
-        p, row0, rows, splits);
-    sample_finish_kernel<kBf16><<<rows, kRowThreads, 0, stream>>>(p, row0, splits);
+    sample_place_kernel<<<rows, kFilterThreads, 0, stream>>>(p, row0, splits);
+    if (p.top_k) {
+      sample_finish_kernel<kBf16, NV, true><<<rows, kRowThreads, 0, stream>>>(p, row0, splits);
+    } else {
+      sample_filter_kernel<kBf16, NV>
+          <<<rows * splits * (kScanThreads / kFilterThreads), kFilterThreads, 0, stream>>>(p, row0, rows, splits);
+      sample_finish_kernel<kBf16, NV, false><<<rows, kRowThreads, 0, stream>>>(p, row0, splits);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -1302,7 +1418,7 @@ hipError_t launch_sample_nv(const SampleParams& p, int splits, hipStream_t strea
 
 template <bool kBf16>
 hipError_t launch_sample_type(const SampleParams& p, hipStream_t stream) {
-  const Shape sh = sample_shape(p.R, p.V, kBf16);
+  const Shape sh = sample_shape(p.R, p.V, kBf16, row_skew(p));
   switch (sh.nv) {
     case 1: return launch_sample_nv<kBf16, 1>(p, sh.splits, stream);
     case 2: return launch_sample_nv<kBf16, 2>(p, sh.splits, stream);
@@ -1315,13 +1431,12 @@ hipError_t launch_sample_type(const SampleParams& p, hipStream_t stream) {
 
 }  // namespace
 
-// One size for both types: an fp32 row has more splits.  Grows with R: rows are spread
-// over at most min(512, 16 R) workgroups or take the splits of 32 tokens per thread.
+// One size for both types: an fp32 row has more splits.  Grows with R: a row is spread
+// over at most 8 workgroups or takes the splits of 32 tokens per thread.
 size_t sample_workspace_bytes(int R, int V) {
   const size_t rows = R < kRowsPerLaunch ? R : kRowsPerLaunch;
-  const size_t whole = rows * ((V + 6) / 4 / (kScanThreads * 8) + 1);
-  const size_t spread = rows < 32 ? 16 * rows : 512;
-  return rows * (sizeof(RowPart) + 256) + (whole > spread ? whole : spread) * sizeof(SplitPart);
+  const size_t whole = (V + 6) / 4 / (kScanThreads * 8) + 1;
+  return rows * sample_part_bytes(static_cast<int>(whole > 8 ? whole : 8));
 }
 
 hipError_t launch_sample(const SampleParams& p, hipStream_t stream) {

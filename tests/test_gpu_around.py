@@ -206,7 +206,7 @@ def test_sample_crowded(gpu, spread, dtype):
 
 
 @pytest.mark.parametrize("R,V,dtype", [(33, 1023, torch.bfloat16), (257, 4097, torch.float32), (1100, 515, torch.float32),
-                                       (2, 262147, torch.bfloat16), (1, 1 << 20, torch.float32)])
+                                       (2, 262147, torch.bfloat16), (1, 1000000, torch.float32)])
 def test_sample_shapes(gpu, R, V, dtype):
     """Rows spread over one to many workgroups, more rows than one launch takes, every row start's alignment."""
     rng = np.random.default_rng(V)
