@@ -112,15 +112,15 @@ __global__ void quantize_q4_kernel(const void* __restrict__ w, size_t groups, ui
 // that are routed to e in node order (deterministic) and one item (expert, first row,
 // rows) per run of its rows.
 // ---------------------------------------------------------------------------
-template <int KMAX>
-__global__ __launch_bounds__(256) void q4_dispatch_kernel(ForwardParams p) {
+template <int KMAX, int kThreads>
+__global__ __launch_bounds__(kThreads) void q4_dispatch_kernel(ForwardParams p) {
   __shared__ int s_cnt[kMaxExperts];
-  __shared__ int s_wave[4];
+  __shared__ int s_wave[kThreads / kWave];
   __shared__ int s_off, s_item;
   const int tid = threadIdx.x, E = p.E, k = p.k, T = p.T, e = blockIdx.x;
-  for (int i = tid; i < E; i += 256) s_cnt[i] = 0;
+  for (int i = tid; i < E; i += kThreads) s_cnt[i] = 0;
   __syncthreads();
-  for (int t = tid; t < T; t += 256) {
+  for (int t = tid; t < T; t += kThreads) {
     int ev[KMAX];
     const uint32_t valid = load_route_row<KMAX>(p.topk_idx + static_cast<size_t>(t) * k, k, E, ev);
 #pragma unroll
@@ -147,10 +147,10 @@ __global__ __launch_bounds__(256) void q4_dispatch_kernel(ForwardParams p) {
   const int count = s_cnt[e], off = s_off;
   if (count == 0) return;
   const int rows = q4_item_rows(count);
-  for (int m = tid; m < q4_items(count); m += 256)
+  for (int m = tid; m < q4_items(count); m += kThreads)
     p.items[s_item + m] = make_int4(e, off + rows * m, min(rows, count - rows * m), 0);
   int seen = 0;
-  for (int t0 = 0; seen < count; t0 += 256) {  // ends at T at the latest: `count` rows hold e
+  for (int t0 = 0; seen < count; t0 += kThreads) {  // ends at T at the latest: `count` rows hold e
     const int t = t0 + tid;
     int slot = -1;
     if (t < T) {
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256) void q4_dispatch_kernel(ForwardParams p) {
     __syncthreads();
     int before = seen + popc64(m & lanes_below(lane_id()));
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < kThreads / kWave; ++w) {
       before += w < wave_id() ? s_wave[w] : 0;
       seen += s_wave[w];
     }
@@ -204,14 +204,15 @@ struct Q4Chunk {
   uint32_t scale;
 };
 
+template <int kPolicy>
 __device__ __forceinline__ Q4Chunk load_q4(const uint4* base, int bytes, int kc, int lane) {
   Q4Chunk c;
 #pragma unroll
   for (int f = 0; f < 4; ++f)
-    c.code[f] = load_weight<kPolicyStream>(base, bytes, kc * (kQ4QuadBytes / 16) + f * kWave + lane);
+    c.code[f] = load_weight<kPolicy>(base, bytes, kc * (kQ4QuadBytes / 16) + f * kWave + lane);
   __amdgpu_buffer_rsrc_t r =
       __builtin_amdgcn_make_buffer_rsrc(const_cast<uint4*>(base), static_cast<short>(0), bytes, kBufferWord3);
-  c.scale = __builtin_amdgcn_raw_buffer_load_b32(r, kc * kQ4QuadBytes + 4096 + lane * 4, 0, kPolicyStream);
+  c.scale = __builtin_amdgcn_raw_buffer_load_b32(r, kc * kQ4QuadBytes + 4096 + lane * 4, 0, kPolicy);
   return c;
 }
 
@@ -238,7 +239,9 @@ __device__ __forceinline__ uint32_t word(const uint4& v, int s) { return s == 0 
 // wave that uses them; the item's rows are staged in LDS, KS chunks a stage, for
 // the four waves.
 // ---------------------------------------------------------------------------
-constexpr int kQ4LdsPieces = 4096;  // 64 KiB: two workgroups per CU
+// LDS pieces of 16 B: two stages of 64 rows; gate/up 32 KiB, four workgroups' worth per CU, down (two planes) 64
+template <bool kDown>
+constexpr int kQ4LdsPieces = kDown ? 4096 : 2048;
 
 struct Q4Rows {
   int slot[kQ4ItemRows];
@@ -247,7 +250,7 @@ struct Q4Rows {
 
 // most M-tiles of a pass: rows of KS chunks and their planes in half of the LDS
 template <bool kDown, int KS>
-constexpr int kQ4MaxTiles = 8 / KS / (kDown ? 2 : 1);
+constexpr int kQ4MaxTiles = 4 / KS;
 
 template <bool kDown, int MT, int KS>
 __device__ __forceinline__ void q4_rows(const ForwardParams& p, int e, int row0, int rows, int m0, int run, uint4* lds,
@@ -255,7 +258,7 @@ __device__ __forceinline__ void q4_rows(const ForwardParams& p, int e, int row0,
   constexpr int kPlanes = kDown ? 2 : 1;
   constexpr int kLoads = KS * kPlanes * MT;  // 16-byte row pieces per thread and stage
   constexpr int kBuf = kLoads * 256;
-  static_assert(2 * kBuf <= kQ4LdsPieces, "two stages fit");
+  static_assert(2 * kBuf <= kQ4LdsPieces<kDown>, "two stages fit");
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));  // keeps address arithmetic of one tile count out of the others
   const int wave = wave_id(), lane = lane_id();
@@ -273,13 +276,14 @@ __device__ __forceinline__ void q4_rows(const ForwardParams& p, int e, int row0,
   // thread tid loads piece tid % 16 (8 columns) of rows tid / 16 + 16 mt
   const int piece = tid & 15, srow = tid >> 4;
   const int plane_pieces = KC * (kQ4Chunk / 8);
-  const uint4* xrow[MT];
+  const uint4* xbase = static_cast<const uint4*>(kDown ? p.act : p.hidden);
+  uint32_t xrow[MT];  // pieces: fewer than 2^32 (checked by the caller)
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int m = m0 + mt * 16 + srow;
     const int row = row0 + (m < rows ? m : 0);  // rows past the item's last read its first; their outputs are dropped
-    xrow[mt] = kDown ? static_cast<const uint4*>(p.act) + static_cast<size_t>(row) * 2 * plane_pieces
-                     : static_cast<const uint4*>(p.hidden) + static_cast<size_t>(p.ent_slot[row] / p.k) * (p.H / 8);
+    xrow[mt] = kDown ? static_cast<uint32_t>(row) * (2 * plane_pieces)
+                     : static_cast<uint32_t>(p.ent_slot[row] / p.k) * (p.H / 8);
   }
   const int nst = (KC + KS - 1) / KS;
   uint4 ra[KS][kPlanes][MT];
@@ -291,7 +295,7 @@ __device__ __forceinline__ void q4_rows(const ForwardParams& p, int e, int row0,
 #pragma unroll
       for (int pl = 0; pl < kPlanes; ++pl)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) ra[c][pl][mt] = xrow[mt][pl * plane_pieces + at];
+        for (int mt = 0; mt < MT; ++mt) ra[c][pl][mt] = xbase[xrow[mt] + (pl * plane_pieces + at)];
     }
   };
   // row `srow`'s piece sits at piece ^ row, so the 16 pieces of a row, and the 16
@@ -342,7 +346,7 @@ __device__ __forceinline__ void q4_rows(const ForwardParams& p, int e, int row0,
   // requested, then stage i is multiplied.
   Q4Chunk wb[2];
   load_rows(0);
-  wb[0] = load_q4(w, wbytes, ks, lane);
+  wb[0] = load_q4<kPolicyPlain>(w, wbytes, ks, lane);
   store_rows(0, 0);
   load_rows(1);
   __syncthreads();
@@ -350,7 +354,7 @@ __device__ __forceinline__ void q4_rows(const ForwardParams& p, int e, int row0,
     constexpr int c = decltype(cur)::value;
     store_rows(i + 1, c ^ 1);
     load_rows(i + 2);
-    wb[c ^ 1] = load_q4(w, wbytes, (i + 1) * KS + ks, lane);  // past the run: zeros
+    wb[c ^ 1] = load_q4<kPolicyPlain>(w, wbytes, (i + 1) * KS + ks, lane);  // past the run: zeros
     __builtin_amdgcn_sched_barrier(0);
     multiply(c, wb[c]);
     __syncthreads();
@@ -362,7 +366,7 @@ __device__ __forceinline__ void q4_rows(const ForwardParams& p, int e, int row0,
     if (++i == nst) break;
   }
   if constexpr (KS > 1) {
-    static_assert((KS - 1) * (4 / KS) * 4 * MT * kWave <= kQ4LdsPieces, "the other waves' sums fit");
+    static_assert((KS - 1) * (4 / KS) * 4 * MT * kWave <= kQ4LdsPieces<kDown>, "the other waves' sums fit");
     floatx4* red = reinterpret_cast<floatx4*>(lds) + (wave / KS) * (KS - 1) * 4 * MT * kWave + lane;
     if (ks > 0) {
 #pragma unroll
@@ -438,17 +442,19 @@ __device__ __forceinline__ void q4_rows(const ForwardParams& p, int e, int row0,
   }
 }
 
-// Workgroups of one item are neighbours on one XCD (workgroup b runs on XCD b % 8),
-// so its rows are read from that XCD's L2.
+// Workgroup b runs on XCD b % 8.  Two neighbouring items, mostly of one expert, share an
+// XCD and take the same run at the same time, so the second one's weights come from its L2;
+// an item's runs follow each other there, so its rows do.
 template <bool kDown, int KS>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void q4_kernel(ForwardParams p, int runs) {
-  __shared__ uint4 lds[kQ4LdsPieces];
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kDown ? 2 : 3))) void q4_kernel(ForwardParams p,
+                                                                                                    int runs) {
+  __shared__ uint4 lds[kQ4LdsPieces<kDown>];
   __shared__ Q4Rows qr;
   const int n_items = *p.n_items;
   const int slot = blockIdx.x / 8;
-  const int item = slot / runs * 8 + blockIdx.x % 8;
+  const int item = (slot / 2 / runs * 8 + blockIdx.x % 8) * 2 + (slot & 1);
   if (item >= n_items) return;
-  const int run = slot % runs;
+  const int run = slot / 2 % runs;
   const int4 d = p.items[item];
   const int e = __builtin_amdgcn_readfirstlane(d.x);
   const int row0 = __builtin_amdgcn_readfirstlane(d.y);
@@ -464,8 +470,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void q
     if (m0 > 0) __syncthreads();  // the rows before have left the LDS
     if (mt == 1) q4_rows<kDown, 1, KS>(p, e, row0, rows, m0, run, lds, qr);
     else if (kMax <= 2 || mt == 2) q4_rows<kDown, (kMax < 2 ? kMax : 2), KS>(p, e, row0, rows, m0, run, lds, qr);
-    else if (kMax <= 4 || mt <= 4) q4_rows<kDown, (kMax < 4 ? kMax : 4), KS>(p, e, row0, rows, m0, run, lds, qr);
-    else if (mt <= 6) q4_rows<kDown, (kMax < 6 ? kMax : 6), KS>(p, e, row0, rows, m0, run, lds, qr);
+    else if (kMax == 3 || mt == 3) q4_rows<kDown, (kMax < 3 ? kMax : 3), KS>(p, e, row0, rows, m0, run, lds, qr);
     else q4_rows<kDown, kMax, KS>(p, e, row0, rows, m0, run, lds, qr);
   }
 }
@@ -474,7 +479,7 @@ template <bool kDown>
 hipError_t launch_q4_pass(const ForwardParams& p, int max_items, hipStream_t stream) {
   const int quads = kDown ? q4_down_quads(p.H) : q4_gate_up_quads(p.I);
   const int runs = (quads + 3) / 4;
-  const long long grid = 8ll * ((max_items + 7) / 8) * runs;
+  const long long grid = 16ll * ((max_items + 15) / 16) * runs;
   if (grid > 0x7fffffffll) return hipErrorInvalidValue;  // far beyond one device's memory
   q4_kernel<kDown, 1><<<static_cast<unsigned>(grid), 256, 0, stream>>>(p, runs);
   return hipGetLastError();
@@ -482,7 +487,8 @@ hipError_t launch_q4_pass(const ForwardParams& p, int max_items, hipStream_t str
 
 template <int KMAX>
 hipError_t launch_q4_dispatch(const ForwardParams& p, hipStream_t stream) {
-  q4_dispatch_kernel<KMAX><<<p.E, 256, 0, stream>>>(p);
+  if (p.T <= 256) q4_dispatch_kernel<KMAX, 256><<<p.E, 256, 0, stream>>>(p);
+  else q4_dispatch_kernel<KMAX, 1024><<<p.E, 1024, 0, stream>>>(p);
   return hipGetLastError();
 }
 

@@ -8,7 +8,7 @@ namespace amoe {
 constexpr int kQ4Group = 32;    // K columns per scale
 constexpr int kQ4Chunk = 128;   // K columns of a weight fragment (16 rows): 64 lanes x 16 B of codes
 constexpr int kQ4QuadBytes = 4 * 1024 + 256;  // four fragments of a chunk and their scales
-constexpr int kQ4ItemRows = 128;
+constexpr int kQ4ItemRows = 64;
 
 constexpr int q4_chunks(int K) { return (K + kQ4Chunk - 1) / kQ4Chunk; }
 // quads of 16-row tiles: gate 2p, gate 2p + 1, up 2p, up 2p + 1; four tiles of the down projection
