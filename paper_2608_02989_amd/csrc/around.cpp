@@ -242,10 +242,9 @@ int32_t acceptmoe_moe_forward_q4(const void* hidden, const void* w_gate_up, cons
   if (k < 1 || k > ACCEPTMOE_MAX_TOPK)
     return fail(ACCEPTMOE_ERR_UNSUPPORTED, "forward_q4: k must be in [1, %d] (got %d)", ACCEPTMOE_MAX_TOPK, k);
   if (T == 0) return ACCEPTMOE_OK;
-  // rows of hidden and of the activations (two planes of I rounded up to 128) are addressed in 32 bits of 16 bytes
-  if (static_cast<long long>(T) * k > (1ll << 30) || static_cast<long long>(T) * H >= (1ll << 35) ||
-      static_cast<long long>(T) * k * 2 * ((I + 127) / 128 * 128) >= (1ll << 35))
-    return fail(ACCEPTMOE_ERR_UNSUPPORTED, "forward_q4: T too large (T=%d k=%d H=%d I=%d)", T, k, H, I);
+  if (static_cast<long long>(T) * k > (1ll << 30) || static_cast<long long>(T) * H >= (1ll << 31) - 8)
+    return fail(ACCEPTMOE_ERR_UNSUPPORTED, "forward_q4: T too large: hidden is addressed in 32 bits (T=%d k=%d H=%d)", T,
+                k, H);
   if (static_cast<long long>((H / 4 + 255) / 256) * T >= (1ll << 31))
     return fail(ACCEPTMOE_ERR_UNSUPPORTED, "forward_q4: T * ceil(H / 1024) must stay below 2^31 (T=%d H=%d)", T, H);
   if (!hidden || !w_gate_up || !w_down || !topk_idx || !topk_gate || !out)

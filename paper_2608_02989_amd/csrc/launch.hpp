@@ -85,7 +85,7 @@ struct ForwardParams {
   int32_t* n_rows;    // [1] dispatched slots (column path)
   int T, H, I, E, k, is_bf16;
   int zero_out;       // gate/up pass clears out (the down pass then adds two halves into it)
-  int item_rows;      // most rows of a column-tile down item (16 per M-tile)
+  int item_rows;      // most rows of a column-tile down item (16 per M-tile), of an item with 4-bit weights
 };
 
 // grouped GEMMs of larger blocks (grouped.hip), both passes
@@ -154,6 +154,6 @@ hipError_t launch_quantize_q4(const void* w, int is_bf16, size_t groups, uint8_t
                               hipStream_t stream);
 size_t forward_q4_workspace_bytes(int T, int H, int I, int E, int k);
 void forward_q4_carve(void* ws, ForwardParams& p);
-hipError_t launch_forward_q4(const ForwardParams& p, hipStream_t stream);
+hipError_t launch_forward_q4(ForwardParams p, hipStream_t stream);
 
 }  // namespace amoe

@@ -112,27 +112,60 @@ __global__ void quantize_q4_kernel(const void* __restrict__ w, size_t groups, ui
 // that are routed to e in node order (deterministic) and one item (expert, first row,
 // rows) per run of its rows.
 // ---------------------------------------------------------------------------
+constexpr int kDispatchSlots = 16384;  // routing entries of a chunk in LDS
+constexpr uint16_t kNoExpert = 0xffff;
+
 template <int KMAX, int kThreads>
 __global__ __launch_bounds__(kThreads) void q4_dispatch_kernel(ForwardParams p) {
   __shared__ int s_cnt[kMaxExperts];
+  __shared__ uint16_t s_idx[kDispatchSlots];
   __shared__ int s_wave[kThreads / kWave];
   __shared__ int s_off, s_item;
   const int tid = threadIdx.x, E = p.E, k = p.k, T = p.T, e = blockIdx.x;
-  for (int i = tid; i < E; i += kThreads) s_cnt[i] = 0;
-  __syncthreads();
-  for (int t = tid; t < T; t += kThreads) {
-    int ev[KMAX];
-    const uint32_t valid = load_route_row<KMAX>(p.topk_idx + static_cast<size_t>(t) * k, k, E, ev);
+  const int per_chunk = kDispatchSlots / k;  // rows
+  // entries outside [0, E), and repeats within a row, as kNoExpert
+  auto load = [&](int t0, int rows) {
+    const int n = rows * k;
+    const int32_t* idx = p.topk_idx + static_cast<size_t>(t0) * k;
+    for (int i0 = tid; i0 < n; i0 += 4 * kThreads) {
+      int v[4];
 #pragma unroll
-    for (int j = 0; j < KMAX; ++j)
-      if (valid & (1u << j)) atomicAdd(&s_cnt[ev[j]], 1);
+      for (int u = 0; u < 4; ++u) v[u] = i0 + u * kThreads < n ? idx[i0 + u * kThreads] : -1;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (i0 + u * kThreads < n)
+          s_idx[i0 + u * kThreads] = v[u] >= 0 && v[u] < E ? static_cast<uint16_t>(v[u]) : kNoExpert;
+    }
+    __syncthreads();
+    for (int r = tid; r < rows; r += kThreads) {
+      uint16_t v[KMAX];
+#pragma unroll
+      for (int j = 0; j < KMAX; ++j) v[j] = s_idx[r * k + min(j, k - 1)];
+#pragma unroll
+      for (int j = 1; j < KMAX; ++j) {
+        bool again = false;
+#pragma unroll
+        for (int d = 0; d < j; ++d) again = again | (v[d] == v[j]);
+        if (again && j < k) s_idx[r * k + j] = kNoExpert;
+      }
+    }
+    __syncthreads();
+  };
+  for (int i = tid; i < E; i += kThreads) s_cnt[i] = 0;
+  for (int t0 = 0; t0 < T; t0 += per_chunk) {
+    const int rows = min(per_chunk, T - t0);
+    load(t0, rows);
+    // Counted along the rows: neighbouring lanes hold one row's experts, which differ, where
+    // the same slot of 64 rows is often one popular expert (64 LDS atomics in a row).
+    for (int i = tid; i < rows * k; i += kThreads)
+      if (s_idx[i] != kNoExpert) atomicAdd(&s_cnt[s_idx[i]], 1);
+    __syncthreads();
   }
-  __syncthreads();
   if (tid < kWave) {
     int off = 0, items = 0;
     for (int e0 = 0; e0 < E; e0 += kWave) {
       const int c = e0 + tid < E ? s_cnt[e0 + tid] : 0;
-      const int n = q4_items(c);
+      const int n = q4_items(c, p.item_rows);
       const int c_incl = wave_incl_scan_i32(c), n_incl = wave_incl_scan_i32(n);
       if (e0 + tid == e) {
         s_off = off + c_incl - c;
@@ -146,30 +179,30 @@ __global__ __launch_bounds__(kThreads) void q4_dispatch_kernel(ForwardParams p) 
   __syncthreads();
   const int count = s_cnt[e], off = s_off;
   if (count == 0) return;
-  const int rows = q4_item_rows(count);
-  for (int m = tid; m < q4_items(count); m += kThreads)
+  const int rows = q4_item_rows(count, p.item_rows);
+  for (int m = tid; m < q4_items(count, p.item_rows); m += kThreads)
     p.items[s_item + m] = make_int4(e, off + rows * m, min(rows, count - rows * m), 0);
   int seen = 0;
-  for (int t0 = 0; seen < count; t0 += kThreads) {  // ends at T at the latest: `count` rows hold e
-    const int t = t0 + tid;
-    int slot = -1;
-    if (t < T) {
-      int ev[KMAX];
-      load_route_row<KMAX>(p.topk_idx + static_cast<size_t>(t) * k, k, E, ev);
+  for (int t0 = 0; t0 < T && seen < count; t0 += per_chunk) {
+    const int n_rows = min(per_chunk, T - t0);
+    if (T > per_chunk) load(t0, n_rows);
+    for (int r0 = 0; r0 < n_rows && seen < count; r0 += kThreads) {
+      const int r = r0 + tid;
+      int slot = -1;
+      if (r < n_rows)
+        for (int j = k - 1; j >= 0; --j) slot = s_idx[r * k + j] == e ? (t0 + r) * k + j : slot;
+      const uint64_t m = __ballot(slot >= 0);
+      if (lane_id() == 0) s_wave[wave_id()] = popc64(m);
+      __syncthreads();
+      int before = seen + popc64(m & lanes_below(lane_id()));
 #pragma unroll
-      for (int j = KMAX - 1; j >= 0; --j) slot = ev[j] == e ? t * k + j : slot;
+      for (int w = 0; w < kThreads / kWave; ++w) {
+        before += w < wave_id() ? s_wave[w] : 0;
+        seen += s_wave[w];
+      }
+      if (slot >= 0) p.ent_slot[off + before] = slot;
+      __syncthreads();
     }
-    const uint64_t m = __ballot(slot >= 0);
-    if (lane_id() == 0) s_wave[wave_id()] = popc64(m);
-    __syncthreads();
-    int before = seen + popc64(m & lanes_below(lane_id()));
-#pragma unroll
-    for (int w = 0; w < kThreads / kWave; ++w) {
-      before += w < wave_id() ? s_wave[w] : 0;
-      seen += s_wave[w];
-    }
-    if (slot >= 0) p.ent_slot[off + before] = slot;
-    __syncthreads();
   }
 }
 
@@ -216,6 +249,15 @@ __device__ __forceinline__ Q4Chunk load_q4(const uint4* base, int bytes, int kc,
   return c;
 }
 
+// 16 bytes at byte `offset` of [base, base + bytes), zeros outside
+__device__ __forceinline__ uint4 load_piece(const void* base, uint32_t bytes, uint32_t offset) {
+  typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+  __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), static_cast<short>(0),
+                                                               static_cast<int>(bytes), kBufferWord3);
+  const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, static_cast<int>(offset), 0, kPolicyPlain);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+
 // eight codes (low nibble first) times the scale, in bf16: exact for scale bytes 2 .. 252
 __device__ __forceinline__ bf16x8 expand_q4(uint32_t codes, float scale) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -233,84 +275,85 @@ __device__ __forceinline__ float scale_of(uint32_t scales, int f) {
 __device__ __forceinline__ uint32_t word(const uint4& v, int s) { return s == 0 ? v.x : s == 1 ? v.y : s == 2 ? v.z : v.w; }
 
 // ---------------------------------------------------------------------------
-// Grouped products.  A workgroup of 4 waves takes one item (expert, up to
-// kQ4ItemRows of its rows) and 4 / KS quads; KS waves share a quad, each over
-// every KS-th chunk of K.  Weights stream straight into the registers of the one
-// wave that uses them; the item's rows are staged in LDS, KS chunks a stage, for
-// the four waves.
+// Grouped products.  A workgroup of NW waves (4, or 2 for small blocks) takes one item
+// (expert, some of its rows) and NW quads, one per wave.  Weights stream straight into the
+// registers of the one wave that uses them; the item's rows are staged in LDS, once
+// for the waves.  (K shared by two or four waves per quad, for blocks of few items:
+// 92 -> 117 us on 64 tokens of the wide layer, every workgroup stages the rows again.)
 // ---------------------------------------------------------------------------
-// LDS pieces of 16 B: two stages of 64 rows; gate/up 32 KiB, four workgroups' worth per CU, down (two planes) 64
-template <bool kDown>
-constexpr int kQ4LdsPieces = kDown ? 4096 : 2048;
+constexpr int kQ4MaxRows = 64;
+// LDS pieces of 16 B: two stages of an item's rows (down: in two planes)
+template <bool kDown, int kRows>
+constexpr int kQ4LdsPieces = 2 * (kDown ? 2 : 1) * kRows * 16;
 
 struct Q4Rows {
-  int slot[kQ4ItemRows];
-  float gate[kQ4ItemRows];
+  int slot[kQ4MaxRows];
+  float gate[kQ4MaxRows];
 };
 
-// most M-tiles of a pass: rows of KS chunks and their planes in half of the LDS
-template <bool kDown, int KS>
-constexpr int kQ4MaxTiles = 4 / KS;
-
-template <bool kDown, int MT, int KS>
-__device__ __forceinline__ void q4_rows(const ForwardParams& p, int e, int row0, int rows, int m0, int run, uint4* lds,
+template <bool kDown, int NW, int MT>
+__device__ __forceinline__ void q4_rows(const ForwardParams& p, int e, int row0, int rows, int run, uint4* lds,
                                         const Q4Rows& qr) {
   constexpr int kPlanes = kDown ? 2 : 1;
-  constexpr int kLoads = KS * kPlanes * MT;  // 16-byte row pieces per thread and stage
-  constexpr int kBuf = kLoads * 256;
-  static_assert(2 * kBuf <= kQ4LdsPieces<kDown>, "two stages fit");
+  constexpr int kBuf = kPlanes * MT * 256;
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));  // keeps address arithmetic of one tile count out of the others
   const int wave = wave_id(), lane = lane_id();
   const int r = lane & 15, g = lane >> 4;
-  const int ks = wave % KS;
   const int K = kDown ? p.I : p.H;
   const int KC = q4_chunks(K);
   const int quads = kDown ? q4_down_quads(p.H) : q4_gate_up_quads(p.I);
-  const int quad = run * (4 / KS) + wave / KS;
+  const int quad = run * NW + wave;
   const bool in = quad < quads;
   const size_t run_bytes = q4_quad_run(K);
   const uint4* w = uniform_ptr(reinterpret_cast<const uint4*>(static_cast<const char*>(kDown ? p.w_down : p.w_gate_up) +
                                                               (static_cast<size_t>(e) * quads + (in ? quad : 0)) * run_bytes));
   const int wbytes = in ? static_cast<int>(run_bytes) : 0;
-  // thread tid loads piece tid % 16 (8 columns) of rows tid / 16 + 16 mt
+  // thread tid loads piece tid % 16 (8 columns) of rows tid / 16 + 4 NW s
+  constexpr int kPass = 4 * NW, kPasses = 16 * MT / kPass;
   const int piece = tid & 15, srow = tid >> 4;
-  const int plane_pieces = KC * (kQ4Chunk / 8);
-  const uint4* xbase = static_cast<const uint4*>(kDown ? p.act : p.hidden);
-  uint32_t xrow[MT];  // pieces: fewer than 2^32 (checked by the caller)
+  const uint32_t plane_bytes = KC * (kQ4Chunk * 2);
+  // Rows past the item's last read its first; their outputs are dropped.  Offsets into hidden fit
+  // 32 bits (checked by the caller), those into the activations start at the item's first row.
+  const void* xbase = kDown ? static_cast<const char*>(p.act) + static_cast<size_t>(row0) * 2 * plane_bytes
+                            : static_cast<const char*>(p.hidden);
+  const uint32_t xbytes = kDown ? static_cast<uint32_t>(rows) * 2 * plane_bytes
+                                : static_cast<uint32_t>(p.T) * static_cast<uint32_t>(p.H) * 2;
+  uint32_t xrow[kPasses];
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    const int m = m0 + mt * 16 + srow;
-    const int row = row0 + (m < rows ? m : 0);  // rows past the item's last read its first; their outputs are dropped
-    xrow[mt] = kDown ? static_cast<uint32_t>(row) * (2 * plane_pieces)
-                     : static_cast<uint32_t>(p.ent_slot[row] / p.k) * (p.H / 8);
+  for (int s = 0; s < kPasses; ++s) {
+    const int m = s * kPass + srow, row = m < rows ? m : 0;
+    xrow[s] = (kDown ? static_cast<uint32_t>(row) * 2 * plane_bytes
+                     : static_cast<uint32_t>(p.ent_slot[row0 + row] / p.k) * static_cast<uint32_t>(p.H) * 2) +
+              piece * 16;
   }
-  const int nst = (KC + KS - 1) / KS;
-  uint4 ra[KS][kPlanes][MT];
-  auto load_rows = [&](int st) {
+  // Weights and rows are requested kAhead stages ahead: with few rows the stages are shorter
+  // than the memory's latency and registers are left.
+  constexpr int kAhead = MT == 1 ? 3 : 1;
+  constexpr int kRing = kAhead == 1 ? 1 : kAhead + 1;  // rows in flight, and the stage being stored
+  uint4 ra[kRing][kPlanes][kPasses], first[1][kPlanes][kPasses];
+  // Columns past K lie outside the resource and read as zeros (a select behind the load would
+  // be moved up to it, with a wait).
+  auto load_rows = [&](int st, int slot, auto& to) {
+    const bool valid = st * kQ4Chunk + piece * 8 < K;
 #pragma unroll
-    for (int c = 0; c < KS; ++c) {
-      int at = (st * KS + c) * 16 + piece;
-      at = at * 8 < K ? at : piece * 8 < K ? piece : 0;  // past K: any piece of the row, see store_rows
+    for (int pl = 0; pl < kPlanes; ++pl)
 #pragma unroll
-      for (int pl = 0; pl < kPlanes; ++pl)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) ra[c][pl][mt] = xbase[xrow[mt] + (pl * plane_pieces + at)];
-    }
+      for (int s = 0; s < kPasses; ++s)
+        to[slot % (sizeof(to) / sizeof(to[0]))][pl][s] =
+            load_piece(xbase, xbytes, valid ? xrow[s] + (pl * plane_bytes + st * (kQ4Chunk * 2)) : ~15u);
   };
-  // row `srow`'s piece sits at piece ^ row, so the 16 pieces of a row, and the 16
+  // a row's piece sits at piece ^ row, so the 16 pieces of a row, and the 16
   // rows that a fragment reads at one piece, fall into different banks
-  auto store_rows = [&](int st, int buf) {
+  auto store_rows = [&](int slot, int buf, const auto& from) {
 #pragma unroll
-    for (int c = 0; c < KS; ++c) {
-      const bool valid = ((st * KS + c) * 16 + piece) * 8 < K;
+    for (int pl = 0; pl < kPlanes; ++pl)
 #pragma unroll
-      for (int pl = 0; pl < kPlanes; ++pl)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-          lds[buf * kBuf + (((c * kPlanes + pl) * MT + mt) * 16 + srow) * 16 + (piece ^ srow)] =
-              valid ? ra[c][pl][mt] : make_uint4(0u, 0u, 0u, 0u);
-    }
+      for (int s = 0; s < kPasses; ++s) {
+        const int row = s * kPass + srow;
+        lds[buf * kBuf + (pl * MT * 16 + row) * 16 + (piece ^ (row & 15))] =
+            from[slot % (sizeof(from) / sizeof(from[0]))][pl][s];
+      }
   };
   floatx4 acc[4][MT];
 #pragma unroll
@@ -318,7 +361,7 @@ __device__ __forceinline__ void q4_rows(const ForwardParams& p, int e, int row0,
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) acc[f][mt] = floatx4{0.f, 0.f, 0.f, 0.f};
   auto multiply = [&](int buf, const Q4Chunk& wc) {
-    const uint4* x0 = lds + buf * kBuf + ks * kPlanes * MT * 256 + r * 16;
+    const uint4* x0 = lds + buf * kBuf + r * 16;
     float sc[4];
 #pragma unroll
     for (int f = 0; f < 4; ++f) sc[f] = scale_of(wc.scale, f);
@@ -341,67 +384,56 @@ __device__ __forceinline__ void q4_rows(const ForwardParams& p, int e, int row0,
       }
     }
   };
-  // Stage i: the rows of stage i + 1, loaded one stage earlier, go to the other LDS
-  // buffer, then the rows of stage i + 2 and the weights of stage i + 1 are
-  // requested, then stage i is multiplied.
-  Q4Chunk wb[2];
-  load_rows(0);
-  wb[0] = load_q4<kPolicyPlain>(w, wbytes, ks, lane);
-  store_rows(0, 0);
-  load_rows(1);
+  // Stage i: the rows of stage i + 1 go to the other LDS buffer, then the rows of stage
+  // i + 1 + kAhead and the weights of stage i + kAhead are requested, then stage i is multiplied.
+  Q4Chunk wb[kAhead + 1];
+  load_rows(0, 0, first);
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) {  // in the loop's order: its first waits have to hold for both
+    load_rows(i + 1, i + 1, ra);
+    wb[i] = load_q4<kPolicyPlain>(w, wbytes, i, lane);
+  }
+  store_rows(0, 0, first);
   __syncthreads();
   auto stage = [&](int i, auto cur) {
     constexpr int c = decltype(cur)::value;
-    store_rows(i + 1, c ^ 1);
-    load_rows(i + 2);
-    wb[c ^ 1] = load_q4<kPolicyPlain>(w, wbytes, (i + 1) * KS + ks, lane);  // past the run: zeros
+    store_rows(c + 1, (c & 1) ^ 1, ra);
+    load_rows(i + 1 + kAhead, c + 1 + kAhead, ra);
+    wb[(c + kAhead) % (kAhead + 1)] = load_q4<kPolicyPlain>(w, wbytes, i + kAhead, lane);  // past the run: zeros
     __builtin_amdgcn_sched_barrier(0);
-    multiply(c, wb[c]);
+    multiply(c & 1, wb[c]);
     __syncthreads();
   };
-  for (int i = 0;;) {
+  // whole rounds of the ring without an exit between the stages: with one the compiler moves
+  // values still being loaded from register to register and waits for them
+  constexpr int kRound = kAhead + 1;
+  int i = 0;
+  for (; i + kRound <= KC; i += kRound) {
     stage(i, std::integral_constant<int, 0>{});
-    if (++i == nst) break;
-    stage(i, std::integral_constant<int, 1>{});
-    if (++i == nst) break;
+    stage(i + 1, std::integral_constant<int, 1>{});
+    if constexpr (kRound == 4) {
+      stage(i + 2, std::integral_constant<int, 2>{});
+      stage(i + 3, std::integral_constant<int, 3>{});
+    }
   }
-  if constexpr (KS > 1) {
-    static_assert((KS - 1) * (4 / KS) * 4 * MT * kWave <= kQ4LdsPieces<kDown>, "the other waves' sums fit");
-    floatx4* red = reinterpret_cast<floatx4*>(lds) + (wave / KS) * (KS - 1) * 4 * MT * kWave + lane;
-    if (ks > 0) {
-#pragma unroll
-      for (int f = 0; f < 4; ++f)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) red[((ks - 1) * 4 * MT + f * MT + mt) * kWave] = acc[f][mt];
-    }
-    __syncthreads();
-    if (ks == 0) {
-#pragma unroll
-      for (int c = 0; c < KS - 1; ++c)
-#pragma unroll
-        for (int f = 0; f < 4; ++f)
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            const floatx4 v = red[(c * 4 * MT + f * MT + mt) * kWave];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) acc[f][mt][q] += v[q];
-          }
-    }
-    __syncthreads();
+  if (i < KC) stage(i, std::integral_constant<int, 0>{});
+  if constexpr (kRound == 4) {
+    if (i + 1 < KC) stage(i + 1, std::integral_constant<int, 1>{});
+    if (i + 2 < KC) stage(i + 2, std::integral_constant<int, 2>{});
   }
 
   // Lane (r, g) holds rows 4 g .. 4 g + 3 of column r of each tile.  Each M-tile goes
   // through this wave's part of the LDS, so rows leave in 16-byte pieces.
-  if (ks == 0 && in) {
+  if (in) {
     constexpr int kRowBytes = kDown ? 64 * 4 : 2 * 32 * 2;  // gate/up: 32 columns, hi then lo
     constexpr int kRowPieces = kRowBytes / 16;
     constexpr int kStride = kRowBytes + 16;
     constexpr int kRowsPerStore = kWave / kRowPieces;
-    char* mine = reinterpret_cast<char*>(lds) + (wave / KS) * 16 * kStride;
+    char* mine = reinterpret_cast<char*>(lds) + wave * 16 * kStride;
     const int pc = lane % kRowPieces;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      const int mb = m0 + mt * 16;
+      const int mb = mt * 16;
       if (mb >= rows) break;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -445,17 +477,24 @@ __device__ __forceinline__ void q4_rows(const ForwardParams& p, int e, int row0,
 // Workgroup b runs on XCD b % 8.  Two neighbouring items, mostly of one expert, share an
 // XCD and take the same run at the same time, so the second one's weights come from its L2;
 // an item's runs follow each other there, so its rows do.
-template <bool kDown, int KS>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kDown ? 2 : 3))) void q4_kernel(ForwardParams p,
-                                                                                                    int runs) {
-  __shared__ uint4 lds[kQ4LdsPieces<kDown>];
+struct Q4Share {
+  int item, run;
+};
+__device__ __forceinline__ Q4Share q4_share(int b, int runs) {
+  const int slot = b / 8;
+  return {(slot / 2 / runs * 8 + b % 8) * 2 + (slot & 1), slot / 2 % runs};
+}
+long long q4_grid(int max_items, int runs) { return 16ll * ((max_items + 15) / 16) * runs; }
+
+template <bool kDown, int NW>
+__global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(kDown && NW == 4 ? 2 : 3))) void q4_kernel(
+    ForwardParams p, int quads) {
+  constexpr int kRows = NW == 4 ? 64 : 32;
+  __shared__ uint4 lds[kQ4LdsPieces<kDown, kRows>];
   __shared__ Q4Rows qr;
-  const int n_items = *p.n_items;
-  const int slot = blockIdx.x / 8;
-  const int item = (slot / 2 / runs * 8 + blockIdx.x % 8) * 2 + (slot & 1);
-  if (item >= n_items) return;
-  const int run = slot / 2 % runs;
-  const int4 d = p.items[item];
+  const Q4Share sh = q4_share(blockIdx.x, (quads + NW - 1) / NW);
+  if (sh.item >= *p.n_items) return;
+  const int4 d = p.items[sh.item];
   const int e = __builtin_amdgcn_readfirstlane(d.x);
   const int row0 = __builtin_amdgcn_readfirstlane(d.y);
   const int rows = __builtin_amdgcn_readfirstlane(d.z);
@@ -464,25 +503,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kDown ? 2 :
     qr.slot[threadIdx.x] = s;
     qr.gate[threadIdx.x] = p.topk_gate[s];
   }
-  constexpr int kMax = kQ4MaxTiles<kDown, KS>;
-  for (int m0 = 0; m0 < rows; m0 += 16 * kMax) {
-    const int mt = (rows - m0 + 15) / 16;
-    if (m0 > 0) __syncthreads();  // the rows before have left the LDS
-    if (mt == 1) q4_rows<kDown, 1, KS>(p, e, row0, rows, m0, run, lds, qr);
-    else if (kMax <= 2 || mt == 2) q4_rows<kDown, (kMax < 2 ? kMax : 2), KS>(p, e, row0, rows, m0, run, lds, qr);
-    else if (kMax == 3 || mt == 3) q4_rows<kDown, (kMax < 3 ? kMax : 3), KS>(p, e, row0, rows, m0, run, lds, qr);
-    else q4_rows<kDown, kMax, KS>(p, e, row0, rows, m0, run, lds, qr);
+  if (rows <= 16) q4_rows<kDown, NW, 1>(p, e, row0, rows, sh.run, lds, qr);
+  else if (kRows == 32 || rows <= 32) q4_rows<kDown, NW, 2>(p, e, row0, rows, sh.run, lds, qr);
+  else if constexpr (kRows == 64) {
+    if (rows <= 48) q4_rows<kDown, NW, 3>(p, e, row0, rows, sh.run, lds, qr);
+    else q4_rows<kDown, NW, 4>(p, e, row0, rows, sh.run, lds, qr);
   }
 }
 
-template <bool kDown>
-hipError_t launch_q4_pass(const ForwardParams& p, int max_items, hipStream_t stream) {
+template <bool kDown, int NW>
+hipError_t launch_q4_pass(const ForwardParams& p, hipStream_t stream) {
   const int quads = kDown ? q4_down_quads(p.H) : q4_gate_up_quads(p.I);
-  const int runs = (quads + 3) / 4;
-  const long long grid = 16ll * ((max_items + 15) / 16) * runs;
+  const long long grid = q4_grid(q4_max_items(p.T * p.k, p.E, p.item_rows), (quads + NW - 1) / NW);
   if (grid > 0x7fffffffll) return hipErrorInvalidValue;  // far beyond one device's memory
-  q4_kernel<kDown, 1><<<static_cast<unsigned>(grid), 256, 0, stream>>>(p, runs);
+  q4_kernel<kDown, NW><<<static_cast<unsigned>(grid), NW * kWave, 0, stream>>>(p, quads);
   return hipGetLastError();
+}
+
+template <int NW>
+hipError_t launch_q4_passes(const ForwardParams& p, hipStream_t stream) {
+  const hipError_t err = launch_q4_pass<false, NW>(p, stream);
+  return err != hipSuccess ? err : launch_q4_pass<true, NW>(p, stream);
 }
 
 template <int KMAX>
@@ -551,7 +592,7 @@ static size_t q4_carve(char* c, int T, int H, int I, int E, int k, ForwardParams
   if (p) p->act = c;
   c += align256(slots * 2 * q4_chunks(I) * kQ4Chunk * 2);
   if (p) p->items = reinterpret_cast<int4*>(c);
-  c += align256(static_cast<size_t>(q4_max_items(static_cast<int>(slots), E)) * sizeof(int4));
+  c += align256(static_cast<size_t>(q4_max_items(static_cast<int>(slots), E, q4_item_limit(T))) * sizeof(int4));
   if (p) p->ys = reinterpret_cast<float*>(c);
   c += align256(slots * H * sizeof(float));
   return c - start;
@@ -561,13 +602,11 @@ size_t forward_q4_workspace_bytes(int T, int H, int I, int E, int k) { return q4
 
 void forward_q4_carve(void* ws, ForwardParams& p) { q4_carve(static_cast<char*>(ws), p.T, p.H, p.I, p.E, p.k, &p); }
 
-hipError_t launch_forward_q4(const ForwardParams& p, hipStream_t stream) {
+hipError_t launch_forward_q4(ForwardParams p, hipStream_t stream) {
+  p.item_rows = q4_item_limit(p.T);
   hipError_t err = p.k <= 8 ? launch_q4_dispatch<8>(p, stream) : launch_q4_dispatch<kMaxTopK>(p, stream);
   if (err != hipSuccess) return err;
-  const int max_items = q4_max_items(p.T * p.k, p.E);
-  err = launch_q4_pass<false>(p, max_items, stream);
-  if (err != hipSuccess) return err;
-  err = launch_q4_pass<true>(p, max_items, stream);
+  err = p.T <= kQ4SmallT ? launch_q4_passes<2>(p, stream) : launch_q4_passes<4>(p, stream);
   if (err != hipSuccess) return err;
   return p.k <= 8 ? launch_q4_combine<8>(p, stream) : launch_q4_combine<kMaxTopK>(p, stream);
 }
