@@ -237,15 +237,20 @@ struct Q4Chunk {
   uint32_t scale;
 };
 
+template <int kPolicy = kPolicyStream>
+__device__ __forceinline__ uint32_t load_scales(const uint4* base, int bytes, int offset) {
+  __amdgpu_buffer_rsrc_t r =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint4*>(base), static_cast<short>(0), bytes, kBufferWord3);
+  return __builtin_amdgcn_raw_buffer_load_b32(r, offset, 0, kPolicy);
+}
+
 template <int kPolicy>
 __device__ __forceinline__ Q4Chunk load_q4(const uint4* base, int bytes, int kc, int lane) {
   Q4Chunk c;
 #pragma unroll
   for (int f = 0; f < 4; ++f)
     c.code[f] = load_weight<kPolicy>(base, bytes, kc * (kQ4QuadBytes / 16) + f * kWave + lane);
-  __amdgpu_buffer_rsrc_t r =
-      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint4*>(base), static_cast<short>(0), bytes, kBufferWord3);
-  c.scale = __builtin_amdgcn_raw_buffer_load_b32(r, kc * kQ4QuadBytes + 4096 + lane * 4, 0, kPolicy);
+  c.scale = load_scales<kPolicy>(base, bytes, kc * kQ4QuadBytes + 4096 + lane * 4);
   return c;
 }
 
@@ -329,7 +334,7 @@ __device__ __forceinline__ void q4_rows(const ForwardParams& p, int e, int row0,
   }
   // Weights and rows are requested kAhead stages ahead: with few rows the stages are shorter
   // than the memory's latency and registers are left.
-  constexpr int kAhead = MT == 1 ? 3 : 1;
+  constexpr int kAhead = MT == 1 || (NW == 2 && MT * kPlanes == 2) ? 3 : 1;
   constexpr int kRing = kAhead == 1 ? 1 : kAhead + 1;  // rows in flight, and the stage being stored
   uint4 ra[kRing][kPlanes][kPasses], first[1][kPlanes][kPasses];
   // Columns past K lie outside the resource and read as zeros (a select behind the load would
@@ -487,7 +492,7 @@ __device__ __forceinline__ Q4Share q4_share(int b, int runs) {
 long long q4_grid(int max_items, int runs) { return 16ll * ((max_items + 15) / 16) * runs; }
 
 template <bool kDown, int NW>
-__global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(kDown && NW == 4 ? 2 : 3))) void q4_kernel(
+__global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(!kDown && NW == 4 ? 3 : 2))) void q4_kernel(
     ForwardParams p, int quads) {
   constexpr int kRows = NW == 4 ? 64 : 32;
   __shared__ uint4 lds[kQ4LdsPieces<kDown, kRows>];
@@ -524,6 +529,191 @@ template <int NW>
 hipError_t launch_q4_passes(const ForwardParams& p, hipStream_t stream) {
   const hipError_t err = launch_q4_pass<false, NW>(p, stream);
   return err != hipSuccess ? err : launch_q4_pass<true, NW>(p, stream);
+}
+
+// ---------------------------------------------------------------------------
+// A few tokens (q4_few): latency is what counts, so two launches and no lists.  One
+// routing entry per lane; the experts are the entries that no earlier one repeats, in
+// that order, and the M side of the MFMA is the tokens themselves.
+//   gate/up   a workgroup per (expert, quad), K shared by its waves; for every token
+//             gate * silu(g) * u (zeros where the token is not routed there) in two planes
+//   down      two workgroups per 16 columns over all experts: the chunks of all experts'
+//             K are dealt to their waves, and the sum over the experts happens in the MFMA's
+//             accumulators and then over the waves, in wave order; each adds its half onto the
+//             zeros that gate/up left in out (two additions onto zero commute: deterministic)
+// ---------------------------------------------------------------------------
+struct FewEntries {
+  int e;           // this lane's expert, -1: none, out of range or repeated within its row
+  uint64_t heads;  // lanes that hold an expert for the first time
+};
+__device__ __forceinline__ FewEntries few_entries(const ForwardParams& p) {
+  const int lane = lane_id(), n = p.T * p.k;
+  const int v = lane < n ? p.topk_idx[lane] : -1;
+  const bool in = v >= 0 && v < p.E;
+  uint32_t same = 0;  // entries with this lane's expert
+  for (int i = 0; i < n; ++i) same |= lane_value(v, i) == v ? 1u << i : 0u;
+  const uint32_t before = same & ((1u << (lane & 31)) - 1u);
+  const int row0 = lane / p.k * p.k;  // this row's first entry
+  const bool again = (before >> (row0 & 31)) != 0;
+  return {in && !again ? v : -1, __ballot(in && before == 0)};
+}
+__device__ __forceinline__ int nth_lane(uint64_t m, int n) {
+  for (int i = 0; i < n; ++i) m &= m - 1;
+  return __builtin_ctzll(m);
+}
+
+constexpr int kFewUpWaves = 8, kFewDownWaves = 16;
+
+__global__ __launch_bounds__(kFewUpWaves * kWave) void q4_few_up_kernel(ForwardParams p, int quads) {
+  __shared__ floatx4 s_sum[kFewUpWaves - 1][4][kWave];
+  __shared__ float s_gate[kQ4FewT];
+  const int wave = wave_id(), lane = lane_id(), r = lane & 15, g = lane >> 4;
+  const int item = blockIdx.x / quads, quad = blockIdx.x % quads;
+  const int K = p.H, KC = q4_chunks(K);
+  const uint32_t xbytes = static_cast<uint32_t>(p.T) * p.H * 2;
+  constexpr int kAhead = 2;  // chunks of this wave in flight behind the one multiplied
+  uint4 xb[kAhead][4];
+  auto load_x = [&](int kc, uint4 (&xv)[4]) {
+    const int col = kc * kQ4Chunk + g * kQ4Group;
+    const uint32_t at = col < K && r < p.T ? (static_cast<uint32_t>(r) * K + col) * 2 : ~63u;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) xv[s] = load_piece(p.hidden, xbytes, at + 16 * s);
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) load_x(wave + i * kFewUpWaves, xb[i]);  // needs no expert
+  const FewEntries en = few_entries(p);
+  {
+    float4* out = reinterpret_cast<float4*>(p.out);
+    for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < p.T * p.H / 4; i += gridDim.x * blockDim.x)
+      out[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  if (item >= popc64(en.heads)) return;
+  const int e = lane_value(en.e, nth_lane(en.heads, item));
+  const size_t run_bytes = q4_quad_run(K);
+  const uint4* w = uniform_ptr(reinterpret_cast<const uint4*>(
+      static_cast<const char*>(p.w_gate_up) + (static_cast<size_t>(e) * quads + quad) * run_bytes));
+  const int wbytes = static_cast<int>(run_bytes);
+  floatx4 acc[4] = {};
+  Q4Chunk wb[kAhead];
+  auto multiply = [&](const Q4Chunk& wv, const uint4 (&xv)[4]) {
+#pragma unroll
+    for (int f = 0; f < 4; ++f)
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xv[s]),
+                                                         expand_q4(word(wv.code[f], s), scale_of(wv.scale, f)), acc[f],
+                                                         0, 0, 0);
+  };
+  // chunks wave, wave + waves, ...; past the last one zeros
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) wb[i] = load_q4<kPolicyStream>(w, wbytes, wave + i * kFewUpWaves, lane);
+  for (int kc = wave; kc < KC; kc += kAhead * kFewUpWaves) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      multiply(wb[i], xb[i]);
+      const int next = kc + (i + kAhead) * kFewUpWaves;
+      if (kc + kAhead * kFewUpWaves >= KC) continue;  // no round follows
+      wb[i] = load_q4<kPolicyStream>(w, wbytes, next, lane);
+      load_x(next, xb[i]);
+    }
+  }
+  if (wave > 0) {
+#pragma unroll
+    for (int f = 0; f < 4; ++f) s_sum[wave - 1][f][lane] = acc[f];
+  } else {
+    // the tokens' gates for this expert; NaN marks a token that is not routed here
+    if (lane < kQ4FewT) s_gate[lane] = __uint_as_float(0x7fc00000u);
+    wave_lds_sync();
+    if (en.e == e) s_gate[lane / p.k] = p.topk_gate[lane];
+  }
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int c = 0; c < kFewUpWaves - 1; ++c)
+#pragma unroll
+    for (int f = 0; f < 4; ++f) {
+      const floatx4 v = s_sum[c][f][lane];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) acc[f][q] += v[q];
+    }
+  uint64_t routed = __ballot(en.e == e);  // entries; a bit per token below
+  const int Ipad = q4_chunks(p.I) * kQ4Chunk;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int t = 4 * g + i;
+    if (t >= p.T) continue;
+    const bool here = ((routed >> (t * p.k)) & ((1ull << p.k) - 1)) != 0;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float v = here ? s_gate[t] * silu_mul(acc[j][i], acc[2 + j][i]) : 0.f;
+      const uint16_t hi = float_to_bf16_bits(v);
+      uint16_t* out = static_cast<uint16_t*>(p.act) + (static_cast<size_t>(item) * p.T + t) * 2 * Ipad + quad * 32 + 16 * j + r;
+      out[0] = hi;
+      out[Ipad] = float_to_bf16_bits(v - bf16_bits_to_float(hi));
+    }
+  }
+}
+
+__global__ __launch_bounds__(kFewDownWaves * kWave) void q4_few_down_kernel(ForwardParams p, int quads) {
+  __shared__ floatx4 s_sum[kFewDownWaves][kWave];
+  const int wave = wave_id(), lane = lane_id(), r = lane & 15, g = lane >> 4;
+  const FewEntries en = few_entries(p);
+  const int n_items = popc64(en.heads);
+  const int half = blockIdx.x % 2, f = blockIdx.x / 2 % 4, quad = blockIdx.x / 8;
+  const int KC = q4_chunks(p.I), pairs = n_items * KC;
+  const int first = half ? (pairs + 1) / 2 : 0, last = half ? pairs : (pairs + 1) / 2;
+  const size_t run_bytes = q4_quad_run(p.I);
+  const uint32_t plane = KC * (kQ4Chunk * 2);  // bytes
+  const uint32_t abytes = static_cast<uint32_t>(n_items) * p.T * 2 * plane;
+  floatx4 acc = {};
+  // This half's (expert, chunk) pairs wave, wave + waves, ...  A loop without loads ahead: its two
+  // rounds fetched as straight code, three pairs deep, took 10.7 us instead of 7.5.
+  for (int q = first + wave; q < last; q += kFewDownWaves) {
+    const int item = q / KC, kc = q - item * KC;
+    const int e = lane_value(en.e, nth_lane(en.heads, item));
+    const uint4* base = uniform_ptr(reinterpret_cast<const uint4*>(
+        static_cast<const char*>(p.w_down) + (static_cast<size_t>(e) * quads + quad) * run_bytes +
+        static_cast<size_t>(kc) * kQ4QuadBytes));
+    const uint4 codes = load_weight<kPolicyStream>(base, kQ4QuadBytes, f * kWave + lane);
+    const uint32_t scales = load_scales(base, kQ4QuadBytes, 4096 + lane * 4);
+    const bool in = kc * kQ4Chunk + g * kQ4Group < p.I && r < p.T;
+    const uint32_t at = in ? (static_cast<uint32_t>(item) * p.T + r) * 2 * plane + (kc * kQ4Chunk + g * kQ4Group) * 2 : ~63u;
+    uint4 hi[4], lo[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      hi[s] = load_piece(p.act, abytes, at + 16 * s);
+      lo[s] = load_piece(p.act, abytes, in ? at + plane + 16 * s : at);
+    }
+    const float scale = scale_of(scales, f);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const bf16x8 b = expand_q4(word(codes, s), scale);
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi[s]), b, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo[s]), b, acc, 0, 0, 0);
+    }
+  }
+  s_sum[wave][lane] = acc;
+  __syncthreads();
+  if (wave > 0) return;
+  acc = s_sum[0][lane];
+#pragma unroll
+  for (int c = 1; c < kFewDownWaves; ++c) {
+    const floatx4 v = s_sum[c][lane];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) acc[q] += v[q];
+  }
+  const int col = quad * 64 + f * 16 + r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (4 * g + i < p.T && col < p.H) atomicAdd(p.out + static_cast<size_t>(4 * g + i) * p.H + col, acc[i]);
+}
+
+hipError_t launch_q4_few(const ForwardParams& p, hipStream_t stream) {
+  const int slots = p.T * p.k, items = p.E < slots ? p.E : slots;
+  const int up = q4_gate_up_quads(p.I), down = q4_down_quads(p.H);
+  q4_few_up_kernel<<<items * up, kFewUpWaves * kWave, 0, stream>>>(p, up);
+  q4_few_down_kernel<<<down * 8, kFewDownWaves * kWave, 0, stream>>>(p, down);
+  return hipGetLastError();
 }
 
 template <int KMAX>
@@ -580,6 +770,15 @@ hipError_t launch_quantize_q4(const void* w, int is_bf16, size_t groups, uint8_t
   return hipGetLastError();
 }
 
+// Activation rows: one per routing entry; a few tokens: one per expert and token.
+static size_t q4_act_rows(int T, int E, int k) {
+  const size_t slots = static_cast<size_t>(T) * k;
+  int few = T < kQ4FewT ? T : kQ4FewT;  // the largest such block up to T (a workspace serves smaller ones, too)
+  few = few < kQ4FewSlots / k ? few : kQ4FewSlots / k;
+  const size_t experts = E < few * k ? E : few * k;
+  return slots > experts * few ? slots : experts * few;
+}
+
 // workspace: [n_items], CSR slot ids, activations (two planes,
 // rows padded to whole chunks), items, per-slot output rows
 static size_t q4_carve(char* c, int T, int H, int I, int E, int k, ForwardParams* p) {
@@ -590,7 +789,7 @@ static size_t q4_carve(char* c, int T, int H, int I, int E, int k, ForwardParams
   if (p) p->ent_slot = reinterpret_cast<int32_t*>(c);
   c += align256(sizeof(int32_t) * slots);
   if (p) p->act = c;
-  c += align256(slots * 2 * q4_chunks(I) * kQ4Chunk * 2);
+  c += align256(q4_act_rows(T, E, k) * 2 * q4_chunks(I) * kQ4Chunk * 2);
   if (p) p->items = reinterpret_cast<int4*>(c);
   c += align256(static_cast<size_t>(q4_max_items(static_cast<int>(slots), E, q4_item_limit(T))) * sizeof(int4));
   if (p) p->ys = reinterpret_cast<float*>(c);
@@ -603,6 +802,7 @@ size_t forward_q4_workspace_bytes(int T, int H, int I, int E, int k) { return q4
 void forward_q4_carve(void* ws, ForwardParams& p) { q4_carve(static_cast<char*>(ws), p.T, p.H, p.I, p.E, p.k, &p); }
 
 hipError_t launch_forward_q4(ForwardParams p, hipStream_t stream) {
+  if (q4_few(p.T, p.k)) return launch_q4_few(p, stream);
   p.item_rows = q4_item_limit(p.T);
   hipError_t err = p.k <= 8 ? launch_q4_dispatch<8>(p, stream) : launch_q4_dispatch<kMaxTopK>(p, stream);
   if (err != hipSuccess) return err;

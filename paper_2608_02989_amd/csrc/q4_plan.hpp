@@ -30,6 +30,12 @@ constexpr int q4_items(int count, int limit) {
   return (count + q4_item_rows(count, limit) - 1) / q4_item_rows(count, limit);
 }
 
+// Blocks of up to this many routing entries (and 16 tokens) take two launches without a
+// dispatch: every workgroup finds its expert in the entries itself.
+constexpr int kQ4FewSlots = 32;
+constexpr int kQ4FewT = 16;
+constexpr bool q4_few(int T, int k) { return T <= kQ4FewT && T * k <= kQ4FewSlots; }
+
 // most items of a block of `slots` routing entries: one per active expert and one
 // more per full item
 constexpr int q4_max_items(int slots, int E, int limit) { return (E < slots ? E : slots) + slots / limit; }
