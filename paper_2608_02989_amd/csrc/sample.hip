@@ -65,7 +65,7 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* part) {
   return s;
 }
 
-constexpr int kFastK = 1000;  // largest top_k taken by candidate lists: one sorted candidate per thread
+constexpr int kFastK = 1000;  // largest top_k taken by candidate lists
 
 enum class Mode { Greedy, TopK, Full, Slow };
 
@@ -118,7 +118,7 @@ __device__ __forceinline__ void block_range(uint32_t& high, uint32_t& low, uint3
 // 11 and 10 bits of the key, with the weights (or counts) of each digit summed
 // in LDS.
 // ---------------------------------------------------------------------------
-constexpr int kRowThreads = 1024;
+constexpr int kRowThreads = 512;
 constexpr int kDigit = 11;
 constexpr int kBins = 1 << kDigit;
 
@@ -162,24 +162,27 @@ __device__ Place find_place(const Row<kBf16>& row, const RowRule& rule, uint64_t
       if (w != 0) atomicAdd(&sh.bin[(key >> shift) & ((1u << bits) - 1u)], static_cast<unsigned long long>(w));
     }
     __syncthreads();
-    // thread t holds bins top - 2 t and top - 2 t - 1: running sums from the largest digit on
-    const int top = (1 << bits) - 1 - 2 * tid;
-    const uint64_t a = top >= 0 ? sh.bin[top] : 0, b = top >= 1 ? sh.bin[top - 1] : 0;
-    uint64_t incl = a + b;
+    // a thread holds neighbouring bins, the largest digits first: running sums from there on
+    constexpr int kMine = kBins / kRowThreads;
+    const int top = (1 << bits) - 1 - kMine * tid;
+    uint64_t own = 0;
+    for (int e = 0; e < kMine; ++e) own += top >= e ? sh.bin[top - e] : 0;
+    uint64_t incl = own;
     for (int o = 1; o < kWave; o <<= 1) {
       const uint64_t v = __shfl_up(incl, o);
       if (lane_id() >= o) incl += v;
     }
     if (lane_id() == kWave - 1) sh.part64[wave_id()] = incl;
     __syncthreads();
-    uint64_t base = before + incl - a - b;
+    uint64_t base = before + incl - own;
     for (int w = 0; w < wave_id(); ++w) base += sh.part64[w];
-    if (base < need && base + a >= need) {
-      sh.digit = top;
-      sh.before = base;
-    } else if (base + a < need && base + a + b >= need) {
-      sh.digit = top - 1;
-      sh.before = base + a;
+    for (int e = 0; e < kMine; ++e) {
+      const uint64_t w = top >= e ? sh.bin[top - e] : 0;
+      if (base < need && base + w >= need) {
+        sh.digit = top - e;
+        sh.before = base;
+      }
+      base += w;
     }
     __syncthreads();
     prefix = (prefix << bits) | sh.digit;
@@ -295,13 +298,10 @@ __device__ void sample_row(const SampleParams& p, int r, const Rules& rules, Row
 //     equal logits): `finish` runs sample_row.
 // ---------------------------------------------------------------------------
 constexpr int kScanThreads = 512;    // four workgroups per CU, in different phases
-constexpr int kBlockThreads = 1024;
 constexpr int kCandCap = 1280;      // candidates of a split
-constexpr int kCandMax = 16384;     // candidates of a row (registers of a workgroup)
 constexpr int kGridBins = 1024;     // 32 nats below the largest logit; weights beyond sum to less than 2^20 e^-31
 constexpr int kCopies = 4;          // of each bin, by lane, against LDS atomics on one address
 constexpr int kListCap = 4096;      // tokens of the listed bins
-constexpr int kWaveList = 1024;     // of them, as many as one wave handles
 constexpr int kRowsPerLaunch = 1024;
 constexpr int kMaxSplits = 64;
 constexpr double kPerNat = 32.0;
@@ -599,28 +599,12 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(8)
   }
 }
 
-// one value per thread, descending over the first n threads (n a power of two from 64 on);
-// the other threads' values must be no larger
-__device__ __forceinline__ unsigned long long block_sort(unsigned long long v, int n, unsigned long long* buf) {
-  const int tid = threadIdx.x;
-  for (int run = 2; run <= n; run *= 2) {
-    for (int j = run / 2; j > 0; j /= 2) {
-      unsigned long long o;
-      if (j >= kWave) {
-        __syncthreads();
-        buf[tid] = v;
-        __syncthreads();
-        o = buf[tid ^ j];
-      } else {
-        o = __shfl_xor(v, j);
-      }
-      const bool larger = ((tid & run) == 0) == ((tid & j) == 0);
-      v = larger == (v > o) ? v : o;
-    }
-  }
-  return v;
-}
-
+// ---------------------------------------------------------------------------
+// From here on a workgroup works on one row, once, so its time is latency and, with
+// code that runs once, the fetching of instructions: short loops over LDS instead of
+// unrolled code over registers (an unrolled sort and search took 25 us for 64 rows, 6 us
+// where all rows were done already).
+// ---------------------------------------------------------------------------
 // inclusive running sum over the workgroup, in thread order
 __device__ __forceinline__ double block_scan(double v, double* part) {
   for (int o = 1; o < kWave; o <<= 1) {
@@ -635,46 +619,58 @@ __device__ __forceinline__ double block_scan(double v, double* part) {
   return before + v;
 }
 
-// Orders n listed tokens, one per thread, and gives each its weight and running sum.
-struct Sorted {
-  unsigned long long token;
-  double weight, sum;  // sum includes the token's own
-};
-template <class Weight>
-__device__ __forceinline__ Sorted sort_and_sum(unsigned long long v, int n, unsigned long long* buf, double* part,
-                                               Weight weight) {
-  int size = kWave;
-  while (size < n) size *= 2;
-  const unsigned long long token = block_sort(v, size, buf);
-  const double w = static_cast<int>(threadIdx.x) < n ? weight(order_key(token)) : 0.0;
-  return {token, w, block_scan(w, part)};
+__device__ __forceinline__ unsigned long long wave_sum_u64(unsigned long long v) {
+  auto add = [](double a, double b) {
+    return __longlong_as_double(__double_as_longlong(a) + __double_as_longlong(b));
+  };
+  return static_cast<unsigned long long>(__double_as_longlong(dpp::reduce(__longlong_as_double(v), 0.0, add)));
 }
 
-struct PickShared {
-  unsigned long long fine[kBlockThreads];
-  unsigned long long buf[kBlockThreads];
-  double part[kBlockThreads / kWave];
+// Sum of the weights of the tokens from `token` on (itself and all larger).
+__device__ __forceinline__ unsigned long long sum_through(const unsigned long long* tokens,
+                                                          const unsigned long long* weights, int n,
+                                                          unsigned long long token) {
+  unsigned long long s = 0;
+#pragma unroll 4
+  for (int j = 0; j < n; ++j) s += tokens[j] >= token ? weights[j] : 0;
+  return s;
+}
+
+constexpr int kPlaceThreads = 256;
+constexpr int kPlaceMine = kGridBins / kPlaceThreads;  // neighbouring bins (or sorted tokens) of a thread
+constexpr int kNearMax = 2048;                         // candidates that reach the cut known so far
+static_assert(kFastK <= kGridBins, "a sorted top-k fits the places");
+
+struct PlaceShared {
+  unsigned long long near[kNearMax];
+  unsigned long long token[kGridBins], weight[kGridBins], sum[kGridBins];
+  double part[kPlaceThreads / kWave];
   double value;
-  int part32[2 * kBlockThreads / kWave];
+  unsigned long long most;
+  int counts[2 * kPlaceThreads / kWave];
   int offset[kMaxSplits + 1];  // candidates in front of each split's
   int n, at;
 };
 
-// smallest thread index where `hit` (monotone or not) holds, n if none
-__device__ __forceinline__ int first_thread(bool hit, int n, PickShared& sh) {
+// smallest bin at which `hit` holds, n if none
+__device__ __forceinline__ int first_bin(const bool (&hit)[kPlaceMine], int n, PlaceShared& sh) {
+  int mine = n;
+#pragma unroll
+  for (int e = kPlaceMine - 1; e >= 0; --e) mine = hit[e] ? static_cast<int>(threadIdx.x) * kPlaceMine + e : mine;
+  const uint64_t m = __ballot(mine < n);
   __syncthreads();
   if (threadIdx.x == 0) sh.at = n;
   __syncthreads();
-  const uint64_t m = __ballot(hit);
-  if (m != 0 && lane_id() == 0) atomicMin(&sh.at, wave_id() * kWave + __builtin_ctzll(m));
+  if (m != 0 && lane_id() == __builtin_ctzll(m)) atomicMin(&sh.at, mine);
   __syncthreads();
   return sh.at;
 }
 
-// the value of thread `at`
-__device__ __forceinline__ double thread_value(double v, int at, PickShared& sh) {
+__device__ __forceinline__ double bin_value(const double (&v)[kPlaceMine], int bin, PlaceShared& sh) {
   __syncthreads();
-  if (static_cast<int>(threadIdx.x) == at) sh.value = v;
+#pragma unroll
+  for (int e = 0; e < kPlaceMine; ++e)
+    if (static_cast<int>(threadIdx.x) * kPlaceMine + e == bin) sh.value = v[e];
   __syncthreads();
   return sh.value;
 }
@@ -687,8 +683,7 @@ __device__ __forceinline__ unsigned long long candidate(const RowView& ws, const
 }
 
 // The cut that leaves exactly k of the candidates; at least k have a key >= least.  Keys of
-// bf16 logits differ in their upper half only (below it zeros, or ones if negative).  Empty
-// places are 0, which no mid reaches.
+// bf16 logits differ in their upper half only (below it zeros, or ones if negative).
 template <class CountKeys, class CountTokens>
 __device__ __forceinline__ unsigned long long cut_to(const SampleParams& p, int k, uint32_t least, uint32_t top,
                                                      CountKeys keys, CountTokens tokens) {
@@ -699,123 +694,43 @@ __device__ __forceinline__ unsigned long long cut_to(const SampleParams& p, int 
   return bisect<unsigned long long>(token_order(key, p.V - 1), token_order(key, 0), k, k, tokens);
 }
 
-// Up to 64 EL candidates left: one wave orders them, value e of a lane at place 64 e + lane.
-template <int EL>
-__device__ __forceinline__ void wave_sort(unsigned long long (&v)[EL]) {
-  const int lane = lane_id();
-#pragma unroll
-  for (int run = 2; run <= kWave * EL; run *= 2) {
-#pragma unroll
+// sh.token[0, n) in descending order (n <= kGridBins)
+__device__ __forceinline__ void sort_tokens(int n, PlaceShared& sh) {
+  int size = 2;
+  while (size < n) size *= 2;
+  for (int i = n + threadIdx.x; i < size; i += kPlaceThreads) sh.token[i] = 0;
+  for (int run = 2; run <= size; run *= 2) {
     for (int j = run / 2; j > 0; j /= 2) {
-      if (j >= kWave) {
-#pragma unroll
-        for (int e = 0; e < EL; ++e) {
-          if (e & (j / kWave)) continue;
-          const bool desc = ((e * kWave) & run) == 0;
-          const unsigned long long a = v[e], b = v[e | (j / kWave)];
-          if (desc == (a < b)) {
-            v[e] = b;
-            v[e | (j / kWave)] = a;
-          }
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < EL; ++e) {
-          const unsigned long long o = __shfl_xor(v[e], j);
-          const bool larger = (((e * kWave + lane) & run) == 0) == ((lane & j) == 0);
-          v[e] = larger == (v[e] > o) ? v[e] : o;
+      __syncthreads();
+      for (int q = threadIdx.x; q < size / 2; q += kPlaceThreads) {
+        const int i = 2 * q - (q & (j - 1));
+        const unsigned long long a = sh.token[i], b = sh.token[i + j];
+        if (((i & run) == 0) == (a < b)) {
+          sh.token[i] = b;
+          sh.token[i + j] = a;
         }
       }
     }
   }
+  __syncthreads();
 }
 
-// smallest place of 64 EL at which `hit` holds
-template <int EL>
-__device__ __forceinline__ int wave_first(const bool (&hit)[EL]) {
-#pragma unroll
-  for (int e = 0; e < EL; ++e) {
-    const uint64_t m = __ballot(hit[e]);
-    if (m != 0) return e * kWave + __builtin_ctzll(m);
-  }
-  return EL * kWave;
-}
-template <int EL>
-__device__ __forceinline__ double wave_value(const double (&v)[EL], int place) {
-  double out = 0.0;
-#pragma unroll
-  for (int e = 0; e < EL; ++e) {
-    const double x = __shfl(v[e], place % kWave);
-    out = place / kWave == e ? x : out;
-  }
-  return out;
-}
-
-template <int EL>
-__device__ void wave_pick(const SampleParams& p, int r, const Rules& rules, uint32_t top, int k, unsigned long long (&v)[EL]) {
-  const int lane = lane_id();
-  wave_sort(v);
-  const RowRule rule{top, key_logit(top), rules.tau};
-  double w[EL], sum[EL], before = 0.0;
-#pragma unroll
-  for (int e = 0; e < EL; ++e) {
-    w[e] = v[e] != 0 ? rule.weight(order_key(v[e])) : 0.0;
-    sum[e] = w[e];
-    for (int o = 1; o < kWave; o <<= 1) {
-      const double u = __shfl_up(sum[e], o);
-      if (lane >= o) sum[e] += u;
-    }
-    sum[e] += before;
-    before = __shfl(sum[e], kWave - 1);
-  }
-  bool hit[EL];
-  int keep = k;
-  if (rules.by_p()) {
-    const double want = rules.top_p * before;
-#pragma unroll
-    for (int e = 0; e < EL; ++e) hit[e] = sum[e] >= want;
-    keep = min(keep, wave_first(hit) + 1);
-  }
-  if (rules.by_m()) {
-    const double m = rules.min_p;
-#pragma unroll
-    for (int e = 0; e < EL; ++e) hit[e] = w[e] < m;
-    keep = min(keep, wave_first(hit));
-  }
-  keep = max(keep, 1);
-  const double total = wave_value(sum, keep - 1);
-  const double at = rules.u * total;
-#pragma unroll
-  for (int e = 0; e < EL; ++e) hit[e] = sum[e] > at;
-  const int j = min(wave_first(hit), keep - 1);
-#pragma unroll
-  for (int e = 0; e < EL; ++e) {
-    if (e * kWave + lane != j) continue;
-    p.token[r] = order_index(v[e]);
-    p.prob[r] = static_cast<float>(w[e] / total);
-  }
-}
-
-// What became of a greedy or top-k row: done, left to a workgroup, or more candidates than
-// the lists hold.
-enum class Picked { Done, Block, Slow };
-
-// Candidates of a greedy or top-k row -> token.  Up to 1024 candidates and a top_k of 256
-// the first wave does it all in registers (a workgroup with its barriers took 18 us
-// instead); more are for a workgroup of kBlockThreads (kBlock).
-template <bool kBlock, class Shared>
-__device__ Picked pick_candidates(const SampleParams& p, int r, const Rules& rules, const RowView& ws, int splits, Shared& sh) {
+// Candidates of a greedy or top-k row -> token.  False: the lists do not hold them all.
+__device__ __forceinline__ bool pick_candidates(const SampleParams& p, int r, const Rules& rules, const RowView& ws,
+                                                int splits, PlaceShared& sh) {
   const int tid = threadIdx.x, lane = lane_id();
   // every wave reads the splits' heads, one per lane
   const int ns = lane < splits ? ws.split[lane].n : 0;
   uint32_t top = lane < splits && ns > 0 ? ws.split[lane].top : 0;
-  for (int o = 32; o >= 1; o >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(top, o)));
+  const uint32_t split_cut = lane < splits ? ws.split[lane].cut : 0;
+  auto larger = [](uint32_t a, uint32_t b) { return max(a, b); };
+  top = dpp::reduce(top, 0u, larger);
   const int upto = wave_incl_scan_i32(ns);
   const int n = lane_value(upto, kWave - 1);
-  if (__ballot(ns > kCandCap) != 0 || n > kCandMax) return Picked::Slow;
+  if (__ballot(ns > kCandCap) != 0) return false;
   if (n == 0) {
     if (tid == 0) p.token[r] = -1, p.prob[r] = 0.f;
-    return Picked::Done;
+    return true;
   }
   if (rules.mode == Mode::Greedy) {
     if (tid < kWave) {
@@ -823,167 +738,154 @@ __device__ Picked pick_candidates(const SampleParams& p, int r, const Rules& rul
       for (int o = 32; o >= 1; o >>= 1) best = max(best, __shfl_xor(best, o));
       if (tid == 0) p.token[r] = order_index(best), p.prob[r] = 1.f;
     }
-    return Picked::Done;
+    return true;
   }
   const int k = min(rules.k, n);
   // a split with k candidates of its own: at least k of the row reach its cut
-  uint32_t least = lane < splits && ns >= k ? ws.split[lane].cut : 0;
-  for (int o = 32; o >= 1; o >>= 1) least = max(least, static_cast<uint32_t>(__shfl_xor(least, o)));
+  uint32_t least = dpp::reduce(ns >= k ? split_cut : 0u, 0u, larger);
   if (wave_id() == 0) {
     if (lane < splits) sh.offset[lane + 1] = upto;
-    if (lane == 0) sh.offset[0] = 0;
+    if (lane == 0) sh.offset[0] = sh.n = 0;
   }
-  constexpr int kWaveMine = 16, kWaveK = 256;
-  if (n <= kWaveMine * kWave && k <= kWaveK) {
-    if (kBlock || wave_id() != 0) return Picked::Done;  // no barrier follows
-    wave_lds_sync();
-    unsigned long long mine[kWaveMine];
-#pragma unroll
-    for (int i = 0; i < kWaveMine; ++i) mine[i] = lane + i * kWave < n ? candidate(ws, sh.offset, lane + i * kWave) : 0;
-    const unsigned long long cut = cut_to(
-        p, k, least, top,
-        [&](uint32_t key) {
-          int c = 0;
-#pragma unroll
-          for (int i = 0; i < kWaveMine; ++i)
-            if (i * kWave < n) c += popc64(__ballot(order_key(mine[i]) >= key));
-          return c;
-        },
-        [&](unsigned long long token) {
-          int c = 0;
-#pragma unroll
-          for (int i = 0; i < kWaveMine; ++i)
-            if (i * kWave < n) c += popc64(__ballot(mine[i] >= token));
-          return c;
-        });
-    int at = 0;
-#pragma unroll
-    for (int i = 0; i < kWaveMine; ++i) {
-      const bool in = mine[i] >= cut && mine[i] != 0;
-      const uint64_t m = __ballot(in);
-      if (in) sh.buf[at + popc64(m & lanes_below(lane))] = mine[i];  // k in all
-      at += popc64(m);
-    }
-    wave_lds_sync();
-    if (k <= kWave) {
-      unsigned long long v[1] = {lane < k ? sh.buf[lane] : 0};
-      wave_pick<1>(p, r, rules, top, k, v);
-    } else {
-      unsigned long long v[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = e * kWave + lane < k ? sh.buf[e * kWave + lane] : 0;
-      if (k <= 2 * kWave) {
-        unsigned long long h[2] = {v[0], v[1]};
-        wave_pick<2>(p, r, rules, top, k, h);
-      } else {
-        wave_pick<4>(p, r, rules, top, k, v);
-      }
-    }
-    return Picked::Done;
-  }
-  if constexpr (!kBlock) {
-    return Picked::Block;
-  } else {
+  if (n > kNearMax) {
+    // raise that bound: counts of 1024 equal ranges of keys
+    int* count = reinterpret_cast<int*>(sh.sum);
+    for (int i = tid; i < kGridBins; i += kPlaceThreads) count[i] = 0;
     __syncthreads();
-    constexpr int kMine = kCandMax / kBlockThreads;
-    unsigned long long mine[kMine];
+    const int shift = max(0, 32 - __clz(static_cast<int>(top - least)) - 10);
+    for (int i = tid; i < n; i += kPlaceThreads) {
+      const uint32_t key = order_key(candidate(ws, sh.offset, i));
+      if (key >= least) atomicAdd(&count[(key - least) >> shift], 1);
+    }
+    __syncthreads();
+    int mine = 0, incl[kPlaceMine];
 #pragma unroll
-    for (int i = 0; i < kMine; ++i)
-      mine[i] = tid + i * kBlockThreads < n ? candidate(ws, sh.offset, tid + i * kBlockThreads) : 0;
+    for (int e = 0; e < kPlaceMine; ++e) {
+      mine += count[kGridBins - 1 - (tid * kPlaceMine + e)];
+      incl[e] = mine;
+    }
+    const int front = static_cast<int>(block_scan(mine, sh.part)) - mine;
+    bool hit[kPlaceMine];
+#pragma unroll
+    for (int e = 0; e < kPlaceMine; ++e) hit[e] = front + incl[e] >= k;
+    least += static_cast<uint32_t>(kGridBins - 1 - first_bin(hit, kGridBins - 1, sh)) << shift;
+  }
+  __syncthreads();
+  for (int i = tid; i < n; i += kPlaceThreads) {
+    const unsigned long long v = candidate(ws, sh.offset, i);
+    if (order_key(v) < least) continue;
+    const int at = atomicAdd(&sh.n, 1);
+    if (at < kNearMax) sh.near[at] = v;
+  }
+  __syncthreads();
+  const int m = sh.n;
+  if (m > kNearMax) return false;
+  constexpr int kMine = kNearMax / kPlaceThreads;
+  unsigned long long mine[kMine];  // empty places are 0, which no cut above 0 reaches
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) mine[i] = tid + i * kPlaceThreads < m ? sh.near[tid + i * kPlaceThreads] : 0;
+  unsigned long long cut = 1;
+  if (m > k) {
     int turn = 0;
-    const unsigned long long cut = cut_to(
+    cut = cut_to(
         p, k, least, top,
         [&](uint32_t key) {
           int c = 0;
 #pragma unroll
           for (int i = 0; i < kMine; ++i)
-            if (i * kBlockThreads < n) c += popc64(__ballot(order_key(mine[i]) >= key));
-          return block_count<kBlockThreads>(c, sh.part32, turn++);
+            if (i * kPlaceThreads < m) c += popc64(__ballot(order_key(mine[i]) >= key));
+          return block_count<kPlaceThreads>(c, sh.counts, turn++);
         },
         [&](unsigned long long token) {
           int c = 0;
 #pragma unroll
           for (int i = 0; i < kMine; ++i)
-            if (i * kBlockThreads < n) c += popc64(__ballot(mine[i] >= token));
-          return block_count<kBlockThreads>(c, sh.part32, turn++);
+            if (i * kPlaceThreads < m) c += popc64(__ballot(mine[i] >= token));
+          return block_count<kPlaceThreads>(c, sh.counts, turn++);
         });
-    __syncthreads();
-    if (tid == 0) sh.n = 0;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kMine; ++i)
-      if (mine[i] >= cut && mine[i] != 0) sh.buf[atomicAdd(&sh.n, 1)] = mine[i];  // k in all
-    __syncthreads();
-    const unsigned long long v = tid < k ? sh.buf[tid] : 0;
-    const RowRule rule{top, key_logit(top), rules.tau};
-    const Sorted t = sort_and_sum(v, k, sh.buf, sh.part, [&](uint32_t key) { return rule.weight(key); });
-    int keep = k;
-    if (rules.by_p()) {
-      const double want = rules.top_p * thread_value(t.sum, k - 1, sh);
-      keep = min(keep, first_thread(tid < k && t.sum >= want, k, sh) + 1);
-    }
-    if (rules.by_m())
-      keep = min(keep, first_thread(tid >= k || t.weight < rules.min_p, k, sh));
-    keep = max(keep, 1);
-    const double total = thread_value(t.sum, keep - 1, sh);
-    const double at = rules.u * total;
-    if (tid == first_thread(tid < keep && t.sum > at, keep - 1, sh)) {
-      p.token[r] = order_index(t.token);
-      p.prob[r] = static_cast<float>(t.weight / total);
-    }
-    return Picked::Done;
   }
-}
-
-constexpr int kFilterThreads = 256;
-constexpr int kFilterMine = kGridBins / kFilterThreads;  // neighbouring bins of a thread
-
-struct FilterShared {
-  unsigned long long buf[256];
-  double part[kFilterThreads / kWave];
-  double value;
-  int offset[kMaxSplits + 1];
-  int at, n_cut, n_pick, cut0, pick0;
-};
-
-// smallest bin at which `hit` holds, n if none
-__device__ __forceinline__ int first_bin(const bool (&hit)[kFilterMine], int n, FilterShared& sh) {
-  int mine = n;
-#pragma unroll
-  for (int e = kFilterMine - 1; e >= 0; --e) mine = hit[e] ? static_cast<int>(threadIdx.x) * kFilterMine + e : mine;
-  const uint64_t m = __ballot(mine < n);
   __syncthreads();
-  if (threadIdx.x == 0) sh.at = n;
-  __syncthreads();
-  if (m != 0 && lane_id() == __builtin_ctzll(m)) atomicMin(&sh.at, mine);
-  __syncthreads();
-  return sh.at;
-}
-
-__device__ __forceinline__ double bin_value(const double (&v)[kFilterMine], int bin, FilterShared& sh) {
+  if (tid == 0) sh.n = 0;
   __syncthreads();
 #pragma unroll
-  for (int e = 0; e < kFilterMine; ++e)
-    if (static_cast<int>(threadIdx.x) * kFilterMine + e == bin) sh.value = v[e];
+  for (int i = 0; i < kMine; ++i)
+    if (mine[i] >= cut) sh.token[atomicAdd(&sh.n, 1)] = mine[i];  // k in all
   __syncthreads();
-  return sh.value;
+  // Weights as whole numbers, and each token's sum through it: up to 256 tokens by adding up
+  // all that are larger (a third of the time of sorting 64), more by sorting.
+  const RowRule rule{top, key_logit(top), rules.tau};
+  const bool direct = k <= kPlaceThreads;
+  if (!direct) sort_tokens(k, sh);
+  for (int t = tid; t < k; t += kPlaceThreads) sh.weight[t] = rule.fixed(order_key(sh.token[t]));
+  if (tid == 0) sh.most = 0;
+  __syncthreads();
+  unsigned long long total = 0;
+  if (direct) {
+    if (tid < k) sh.sum[tid] = sum_through(sh.token, sh.weight, k, sh.token[tid]);
+  } else {
+    unsigned long long run[kPlaceMine], s = 0;
+#pragma unroll
+    for (int e = 0; e < kPlaceMine; ++e) {
+      const int t = tid * kPlaceMine + e;
+      s += t < k ? sh.weight[t] : 0;
+      run[e] = s;
+    }
+    unsigned long long upto64 = s;
+    for (int o = 1; o < kWave; o <<= 1) {
+      const unsigned long long u = __shfl_up(upto64, o);
+      if (lane >= o) upto64 += u;
+    }
+    if (lane == kWave - 1) sh.near[wave_id()] = upto64;
+    __syncthreads();
+    unsigned long long front = upto64 - s;
+    for (int w = 0; w < wave_id(); ++w) front += sh.near[w];
+#pragma unroll
+    for (int e = 0; e < kPlaceMine; ++e)
+      if (tid * kPlaceMine + e < k) sh.sum[tid * kPlaceMine + e] = front + run[e];
+  }
+  __syncthreads();
+  // C of the top_k is the largest sum, C of what the other filters keep the largest one kept:
+  // each keeps a prefix, and always the first token (whose sum is its weight)
+  for (int t = tid; t < k; t += kPlaceThreads) total = max(total, sh.sum[t]);
+  if (total != 0) atomicMax(&sh.most, total);
+  __syncthreads();
+  const double want = rules.by_p() ? rules.top_p * static_cast<double>(sh.most) : INFINITY;
+  __syncthreads();
+  if (tid == 0) sh.most = 0;
+  __syncthreads();
+  unsigned long long kept = 0;
+  for (int t = tid; t < k; t += kPlaceThreads) {
+    const unsigned long long w = sh.weight[t], before = sh.sum[t] - w;
+    const bool keep = static_cast<double>(before) < want &&
+                      (!rules.by_m() || rule.weight(order_key(sh.token[t])) >= rules.min_p);
+    if (keep || before == 0) kept = max(kept, sh.sum[t]);
+  }
+  if (kept != 0) atomicMax(&sh.most, kept);
+  __syncthreads();
+  const double c = static_cast<double>(sh.most);
+  const unsigned long long at = min(static_cast<unsigned long long>(rules.u * c), sh.most - 1);
+  for (int t = tid; t < k; t += kPlaceThreads) {
+    if (sh.sum[t] <= at || sh.sum[t] - sh.weight[t] > at) continue;  // one token's sum passes u C
+    p.token[r] = order_index(sh.token[t]);
+    p.prob[r] = static_cast<float>(rule.weight(order_key(sh.token[t])) * kWeightOne / c);
+  }
+  return true;
 }
 
 // One workgroup per row: a greedy or top-k row's token from its candidates, else the bins in
 // which the kept prefix ends and in which the sample lies.
-__global__ __launch_bounds__(kFilterThreads) void sample_place_kernel(SampleParams p, int row0, int splits) {
-  __shared__ FilterShared sh;
+__global__ __launch_bounds__(kPlaceThreads) void sample_place_kernel(SampleParams p, int row0, int splits) {
+  __shared__ PlaceShared sh;
   const int local = blockIdx.x, r = row0 + local, tid = threadIdx.x;
   const RowView ws(p, local, splits);
   const Rules rules = row_rules(p, r);
   if (rules.mode == Mode::Slow) return;
   if (rules.mode != Mode::Full) {
-    const Picked done = pick_candidates<false>(p, r, rules, ws, splits, sh);
-    if (tid == 0 && done != Picked::Done) ws.row->slow = done == Picked::Slow ? 1 : 2;
+    if (!pick_candidates(p, r, rules, ws, splits, sh) && tid == 0) ws.row->slow = 1;
     return;
   }
   uint32_t top = lane_id() < splits ? ws.split[lane_id()].top : 0;
-  for (int o = 32; o >= 1; o >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(top, o)));
+  top = dpp::reduce(top, 0u, [](uint32_t a, uint32_t b) { return max(a, b); });
   const Grid grid{kPerNat / static_cast<double>(rules.tau)};
   const double grid_top = floor(grid.at(top));
   // far from 0 the grid's 64 bits no longer hold the weights' digits
@@ -995,23 +897,22 @@ __global__ __launch_bounds__(kFilterThreads) void sample_place_kernel(SamplePara
   }
   if (top <= kKeyNegInf || slow) return;
   // the row's sums in this thread's bins below its largest logit
-  unsigned long long sum[kFilterMine] = {};
+  unsigned long long sum[kPlaceMine] = {};
   for (int i = 0; i < splits; ++i) {
     const uint32_t part_top = ws.split[i].top;
     if (part_top <= kKeyNegInf) continue;
     const double lower = grid_top - floor(grid.at(part_top));
     if (lower >= kGridBins) continue;
-    const int at = tid * kFilterMine - static_cast<int>(lower);
+    const int at = tid * kPlaceMine - static_cast<int>(lower);
 #pragma unroll
-    for (int e = 0; e < kFilterMine; ++e)
+    for (int e = 0; e < kPlaceMine; ++e)
       if (at + e >= 0) sum[e] += ws.split[i].data[at + e];
   }
-  double incl[kFilterMine], excl[kFilterMine], mine = 0.0;
-  const double base = exp(-tid * kFilterMine / kPerNat) / kWeightOne;
+  double incl[kPlaceMine], excl[kPlaceMine], mine = 0.0;
   constexpr double kStep = 0.96923323447634413;  // exp(-1 / 32)
-  double factor = base;
+  double factor = exp(-tid * kPlaceMine / kPerNat) / kWeightOne;
 #pragma unroll
-  for (int e = 0; e < kFilterMine; ++e) {
+  for (int e = 0; e < kPlaceMine; ++e) {
     excl[e] = mine;
     mine += static_cast<double>(sum[e]) * factor;
     incl[e] = mine;
@@ -1019,15 +920,15 @@ __global__ __launch_bounds__(kFilterThreads) void sample_place_kernel(SamplePara
   }
   const double front = block_scan(mine, sh.part) - mine;
 #pragma unroll
-  for (int e = 0; e < kFilterMine; ++e) {
+  for (int e = 0; e < kPlaceMine; ++e) {
     excl[e] += front;
     incl[e] += front;
   }
   const double total = bin_value(incl, kGridBins - 1, sh);
-  bool hit[kFilterMine];
+  bool hit[kPlaceMine];
   auto first = [&](auto passes, int n) {
 #pragma unroll
-    for (int e = 0; e < kFilterMine; ++e) hit[e] = passes(incl[e]);
+    for (int e = 0; e < kPlaceMine; ++e) hit[e] = passes(incl[e]);
     return min(first_bin(hit, n, sh), n);
   };
   int cut = -1;
@@ -1049,9 +950,9 @@ __global__ __launch_bounds__(kFilterThreads) void sample_place_kernel(SamplePara
   const int pick0 = first([&](double v) { return v > rules.u * least; }, last);
   const int pick1 = kept > least ? first([&](double v) { return v > rules.u * kept; }, last) : pick0;
 #pragma unroll
-  for (int e = 0; e < kFilterMine; ++e) {
-    if (tid * kFilterMine + e == pick0) ws.row->before_pick = excl[e];
-    if (tid * kFilterMine + e == cut) ws.row->before_cut = excl[e];
+  for (int e = 0; e < kPlaceMine; ++e) {
+    if (tid * kPlaceMine + e == pick0) ws.row->before_pick = excl[e];
+    if (tid * kPlaceMine + e == cut) ws.row->before_cut = excl[e];
   }
   if (tid == 0) {
     ws.row->t_cut = cut;
@@ -1115,10 +1016,10 @@ __device__ __forceinline__ void list_tokens(const Pieces<kBf16, NV, kThreads>& z
 }
 
 template <bool kBf16, int NV>
-__global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SampleParams p, int row0, int rows, int splits) {
+__global__ __launch_bounds__(kPlaceThreads) void sample_filter_kernel(SampleParams p, int row0, int rows, int splits) {
   __shared__ FilterCounts sh;
   const int local = blockIdx.x % rows, r = row0 + local, s = blockIdx.x / rows;
-  Pieces<kBf16, NV, kFilterThreads> z;
+  Pieces<kBf16, NV, kPlaceThreads> z;
   z.load(p, r, s);
   const RowView ws(p, local, splits);
   const Rules rules = row_rules(p, r);
@@ -1126,217 +1027,201 @@ __global__ __launch_bounds__(kFilterThreads) void sample_filter_kernel(SamplePar
   list_tokens(z, Grid{kPerNat / static_cast<double>(rules.tau)}, *ws.row, sh);
 }
 
-union FinishShared {
-  RowShared row;
-  PickShared pick;
-};
+constexpr int kFinishMine = kListCap / kRowThreads;
+constexpr int kWindow = 64;  // tokens around a place, ordered by adding up all larger ones
 
-__device__ __forceinline__ unsigned long long wave_sum_u64(unsigned long long v) {
-  auto add = [](double a, double b) {
-    return __longlong_as_double(__double_as_longlong(a) + __double_as_longlong(b));
-  };
-  return static_cast<unsigned long long>(__double_as_longlong(dpp::reduce(__longlong_as_double(v), 0.0, add)));
-}
-
-// A listed range of bins in the registers of a wave (up to 1024 tokens) or a workgroup of
-// kBlockThreads: token and weight, in 2^-43 of the range's first bin (whole numbers: sums in
-// any order are the same).
-template <bool kBlock>
-struct Listed {
-  static constexpr int kThreads = kBlock ? kBlockThreads : kWave;
-  static constexpr int kMine = kBlock ? kListCap / kBlockThreads : kWaveList / kWave;
-  unsigned long long token[kMine], weight[kMine];
-  double unit;  // what 1 of them stands for
+struct FinishShared {
+  unsigned long long token[kWindow], weight[kWindow];
+  double step[kGridBins];  // exp(-b / 32)
+  unsigned long long part64[2 * kRowThreads / kWave];
+  int part32[2 * kRowThreads / kWave];
+  uint32_t range[2 * kRowThreads / kWave];
+  unsigned long long found;
+  double sum;
   int n;
-
-  __device__ __forceinline__ Listed(const unsigned long long* list, int n_) : n(n_) {
-    const int me = kBlock ? static_cast<int>(threadIdx.x) : lane_id();
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) token[i] = me + i * kThreads < n ? list[me + i * kThreads] : 0;
-  }
-  __device__ __forceinline__ void weigh(const Grid& grid, double grid_top, int t0) {
-    unit = exp(-t0 / kPerNat) / kWeightOne;
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      weight[i] = 0;
-      if (i * kThreads >= n) continue;
-      const double g = grid.at(order_key(token[i])), b = floor(g), below = grid_top - t0 - b;
-      double w = Grid::weight(g - b);
-      if (__ballot(token[i] != 0 && below != 0.0) != 0) w *= exp(-below / kPerNat);  // mostly the list is one bin
-      weight[i] = token[i] != 0 ? __double2ull_rn(w * kWeightOne) : 0;
-    }
-  }
 };
 
-struct Sums {
-  unsigned long long weight;
-  int count;
+union FinishUnion {
+  RowShared row;
+  FinishShared fin;
 };
 
-// Sums over the wave, or the workgroup: there one barrier a call, calls in a row alternate
-// between two halves of the shared words.
-template <bool kBlock>
-__device__ __forceinline__ Sums group_sums(unsigned long long w, int c, PickShared& sh, int turn) {
-  w = wave_sum_u64(w);
-  if constexpr (!kBlock) {
-    return {w, c};
-  } else {
-    constexpr int kWaves = kBlockThreads / kWave;
-    const int half = (turn & 1) * kWaves;
-    if (lane_id() == 0) {
-      sh.fine[half + wave_id()] = w;
-      sh.part32[half + wave_id()] = c;
-    }
-    __syncthreads();
-    const int at = half + lane_id() % kWaves;
-    return {wave_sum_u64(lane_id() < kWaves ? sh.fine[at] : 0), wave_sum_i32(lane_id() < kWaves ? sh.part32[at] : 0)};
-  }
-}
+// A listed range of bins in the registers of the workgroup: token and weight, in 2^-43 of
+// the range's first bin (whole numbers: sums in any order are the same).
+struct Listed {
+  unsigned long long token[kFinishMine], weight[kFinishMine];
+  int n;
+};
 
-template <bool kBlock>
-__device__ __forceinline__ void group_sync() {
-  if constexpr (kBlock) __syncthreads();
-  else wave_lds_sync();
-}
-
-// The token of a list at which passes(before + sum up to it) turns true, and that sum; the
-// list's last one if it never does.  The order is searched by halves until at most 64 tokens
-// are left around the place, and those are sorted.
 struct PlaceInList {
   unsigned long long token;
   double sum;
 };
-template <bool kBlock, class Passes>
-__device__ __forceinline__ PlaceInList place_in_list(const Listed<kBlock>& l, double before, PickShared& sh,
+
+// The token of a list, from bin t0 on, at which passes(before + sum up to it) turns true, and that
+// sum; the list's last one if it never does.  The order is searched by halves until at most
+// kWindow tokens are left around the place.
+template <class Passes>
+__device__ __forceinline__ PlaceInList place_in_list(const Listed& l, int t0, double before, FinishShared& sh,
                                                      Passes passes) {
-  const int lane = lane_id();
+  constexpr int kWaves = kRowThreads / kWave;
+  const int tid = threadIdx.x, lane = lane_id();
+  const double unit = sh.step[t0] / kWeightOne;
   // every token lies in [lo, hi): a list's keys share their upper bits
   uint32_t least = ~0u, most = 0;
 #pragma unroll
-  for (int i = 0; i < Listed<kBlock>::kMine; ++i) {
+  for (int i = 0; i < kFinishMine; ++i) {
     least = min(least, l.token[i] != 0 ? order_key(l.token[i]) : ~0u);
     most = max(most, order_key(l.token[i]));
   }
-  if constexpr (kBlock) {
-    block_range(most, least, reinterpret_cast<uint32_t*>(sh.buf));
-  } else {
-    auto larger = [](uint32_t a, uint32_t b) { return max(a, b); };
-    most = dpp::reduce(most, 0u, larger);
-    least = ~dpp::reduce(~least, 0u, larger);
-  }
+  block_range(most, least, sh.range);
   unsigned long long lo = static_cast<unsigned long long>(least) << 32;
   unsigned long long hi = (static_cast<unsigned long long>(most) + 1) << 32;
-  Sums above = {0, 0};  // of tokens from hi on
-  int inside = l.n, turn = 0;
-  while (inside > kWave && hi - lo > 1) {
+  unsigned long long above = 0;  // weight of tokens from hi on
+  int inside = l.n, count_above = 0;
+  for (int turn = 0; inside > kWindow && hi - lo > 1; ++turn) {
     const unsigned long long mid = lo + (hi - lo) / 2;
     unsigned long long w = 0;
     int c = 0;
 #pragma unroll
-    for (int i = 0; i < Listed<kBlock>::kMine; ++i) {
-      if (i * Listed<kBlock>::kThreads >= l.n) continue;
+    for (int i = 0; i < kFinishMine; ++i) {
+      if (i * kRowThreads >= l.n) continue;
       w += l.token[i] >= mid ? l.weight[i] : 0;
       c += popc64(__ballot(l.token[i] >= mid));
     }
-    const Sums s = group_sums<kBlock>(w, c, sh, turn++);
-    if (passes(before + static_cast<double>(s.weight) * l.unit)) {
+    w = wave_sum_u64(w);
+    const int half = (turn & 1) * kWaves;
+    if (lane == 0) {
+      sh.part64[half + wave_id()] = w;
+      sh.part32[half + wave_id()] = c;
+    }
+    __syncthreads();
+    w = 0;
+    c = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      w += sh.part64[half + i];
+      c += sh.part32[half + i];
+    }
+    if (passes(before + static_cast<double>(w) * unit)) {
       lo = mid;
-      inside = s.count - above.count;
+      inside = c - count_above;
     } else {
       hi = mid;
-      inside -= s.count - above.count;
-      above = s;
+      inside -= c - count_above;
+      above = w;
+      count_above = c;
     }
   }
-  group_sync<kBlock>();
-  if (threadIdx.x == 0) sh.n = 0;
-  group_sync<kBlock>();
+  __syncthreads();
+  if (tid == 0) {
+    sh.n = 0;
+    sh.found = ~0ull;
+  }
+  __syncthreads();
 #pragma unroll
-  for (int i = 0; i < Listed<kBlock>::kMine; ++i) {
+  for (int i = 0; i < kFinishMine; ++i) {
     if (l.token[i] == 0 || l.token[i] < lo || l.token[i] >= hi) continue;
-    const int at = atomicAdd(&sh.n, 1);  // 64 at most
-    sh.buf[at] = l.token[i];
-    sh.fine[at] = l.weight[i];
+    const int at = atomicAdd(&sh.n, 1);  // kWindow at most
+    sh.token[at] = l.token[i];
+    sh.weight[at] = l.weight[i];
   }
-  group_sync<kBlock>();
+  __syncthreads();
   const int m = sh.n;
-  unsigned long long v = lane < m ? sh.buf[lane] : 0, w = lane < m ? sh.fine[lane] : 0;
-  group_sync<kBlock>();
-#pragma unroll
-  for (int run = 2; run <= kWave; run *= 2) {
-#pragma unroll
-    for (int j = run / 2; j > 0; j /= 2) {
-      const unsigned long long o = __shfl_xor(v, j), ow = __shfl_xor(w, j);
-      const bool take = (((lane & run) == 0) == ((lane & j) == 0)) != (v > o);
-      v = take ? o : v;
-      w = take ? ow : w;
+  if (tid < kWave) {
+    const unsigned long long v = lane < m ? sh.token[lane] : ~0ull, w = lane < m ? sh.weight[lane] : 0;
+    const unsigned long long s = above + (lane < m ? sum_through(sh.token, sh.weight, m, v) : 0);
+    const double sum = before + static_cast<double>(s) * unit;
+    const bool here = lane < m && passes(sum) && !passes(before + static_cast<double>(s - w) * unit);
+    if (lane < m && __ballot(here) == 0) atomicMin(&sh.found, v);  // none: the smallest
+    wave_lds_sync();
+    if (here || (lane < m && sh.found == v) || (m == 0 && lane == 0)) {
+      sh.found = m == 0 ? 0 : v;
+      sh.sum = m == 0 ? before : sum;
     }
   }
-  for (int o = 1; o < kWave; o <<= 1) {
-    const unsigned long long u = __shfl_up(w, o);
-    if (lane >= o) w += u;
-  }
-  const double sum = before + static_cast<double>(above.weight + w) * l.unit;
-  const uint64_t hit = __ballot(lane < m && passes(sum));
-  const int at = hit != 0 ? __builtin_ctzll(hit) : max(m - 1, 0);
-  return {__shfl(v, at), __shfl(sum, at)};
+  __syncthreads();
+  return {sh.found, sh.sum};
 }
 
-// The token of a row whose bins are listed, by one wave or the workgroup.
-template <bool kBlock>
-__device__ void finish_row(const SampleParams& p, int r, const Rules& rules, const RowPart& in, const RowHead& head,
-                           int n_cut, int n_pick, PickShared& sh) {
+__device__ __forceinline__ int bin_index(double t) { return static_cast<int>(fmin(fmax(t, 0.0), kGridBins - 1.0)); }
+
+// The token of a row whose bins are listed.
+__device__ __forceinline__ void finish_row(const SampleParams& p, int r, const Rules& rules, const RowPart& in,
+                                           const RowHead& head, int n_cut, int n_pick, FinishShared& sh) {
+  const int tid = threadIdx.x;
   const Grid grid{kPerNat / static_cast<double>(rules.tau)};
-  const double grid_top = head.grid_top;
+  for (int b = tid; b < kGridBins; b += kRowThreads) sh.step[b] = exp(-b / kPerNat);
+  __syncthreads();
   double total = head.total;
-  if (head.t_cut >= 0) {
-    // both filters keep a prefix: the shorter one
-    Listed<kBlock> l(in.cut, n_cut);
-    l.weigh(grid, grid_top, head.t_cut);
-    double kept = INFINITY;
-    if (rules.by_p()) {
-      const double want = rules.top_p * total;
-      const PlaceInList at = place_in_list(l, head.before_cut, sh, [&](double sum) { return sum >= want; });
-      if (at.sum >= want) kept = at.sum;
+  unsigned long long token = 0;
+  // first the list in which the kept prefix ends, then that in which the sample lies
+  for (int step = head.t_cut >= 0 ? 0 : 1; step < 2; ++step) {
+    const unsigned long long* list = step == 0 ? in.cut : in.pick;
+    const int t0 = step == 0 ? head.t_cut : head.t_pick0;
+    const double before = step == 0 ? head.before_cut : head.before_pick;
+    Listed l;
+    l.n = step == 0 ? n_cut : n_pick;
+#pragma unroll
+    for (int i = 0; i < kFinishMine; ++i)
+      l.token[i] = tid + i * kRowThreads < l.n ? list[tid + i * kRowThreads] : 0;
+#pragma unroll
+    for (int i = 0; i < kFinishMine; ++i) {
+      l.weight[i] = 0;
+      if (l.token[i] == 0) continue;
+      const double g = grid.at(order_key(l.token[i])), b = floor(g);
+      l.weight[i] = __double2ull_rn(Grid::weight(g - b) * sh.step[bin_index(head.grid_top - t0 - b)] * kWeightOne);
     }
+    // both filters keep a prefix: the shorter one
+    const double want = step == 1 ? rules.u * total : rules.by_p() ? rules.top_p * total : INFINITY;
+    const PlaceInList at = place_in_list(l, t0, before, sh, [&](double sum) { return step == 1 ? sum > want : sum >= want; });
+    if (step == 1) {
+      token = at.token;
+      break;
+    }
+    double kept = at.sum >= want ? at.sum : INFINITY;
     if (rules.by_m()) {
       const RowRule rule{head.top, key_logit(head.top), rules.tau};
-      const double m = rules.min_p;
       unsigned long long w = 0;
+#pragma unroll 1
+      for (int i = 0; i < l.n; i += kRowThreads) {
+        unsigned long long v = 0, own = 0;
 #pragma unroll
-      for (int i = 0; i < Listed<kBlock>::kMine; ++i)
-        if (l.token[i] != 0 && rule.weight(order_key(l.token[i])) >= m) w += l.weight[i];
-      group_sync<kBlock>();
-      kept = fmin(kept, head.before_cut + static_cast<double>(group_sums<kBlock>(w, 0, sh, 0).weight) * l.unit);
-      group_sync<kBlock>();
+        for (int q = 0; q < kFinishMine; ++q) {
+          v = q * kRowThreads == i ? l.token[q] : v;
+          own = q * kRowThreads == i ? l.weight[q] : own;
+        }
+        if (v != 0 && rule.weight(order_key(v)) >= rules.min_p) w += own;
+      }
+      w = wave_sum_u64(w);
+      __syncthreads();
+      if (lane_id() == 0) sh.part64[wave_id()] = w;
+      __syncthreads();
+      w = 0;
+      for (int i = 0; i < kRowThreads / kWave; ++i) w += sh.part64[i];
+      kept = fmin(kept, before + static_cast<double>(w) * (sh.step[t0] / kWeightOne));
+      __syncthreads();
     }
     total = fmin(kept, total);
   }
-  const double at = rules.u * total;
-  Listed<kBlock> l(in.pick, n_pick);
-  l.weigh(grid, grid_top, head.t_pick0);
-  const PlaceInList j = place_in_list(l, head.before_pick, sh, [&](double sum) { return sum > at; });
-  if (threadIdx.x == 0) {
-    const double g = grid.at(order_key(j.token)), b = floor(g);
-    p.token[r] = order_index(j.token);
-    p.prob[r] = static_cast<float>(Grid::weight(g - b) * exp((b - grid_top) / kPerNat) / total);
+  if (tid == 0) {
+    const double g = grid.at(order_key(token)), b = floor(g);
+    p.token[r] = order_index(token);
+    p.prob[r] = static_cast<float>(Grid::weight(g - b) * sh.step[bin_index(head.grid_top - b)] / total);
   }
 }
 
 // A row that is not done yet, by a workgroup.  kList: lists the bins' tokens itself, part after
 // part; used beside top_k, where few rows need it.
 template <bool kBf16, int NV, bool kList>
-__device__ __forceinline__ void finish_one(const SampleParams& p, int row0, int local, int splits, FinishShared& un,
-                                           FilterCounts& counts) {
-  const int r = row0 + local, tid = threadIdx.x;
+__global__ __launch_bounds__(kRowThreads) void sample_finish_kernel(SampleParams p, int row0, int splits) {
+  __shared__ FinishUnion un;
+  __shared__ FilterCounts counts;
+  const int local = blockIdx.x, r = row0 + local, tid = threadIdx.x;
   const RowView ws(p, local, splits);
   RowPart& in = *ws.row;
   const RowHead head = in;
   const Rules rules = row_rules(p, r);
-  if (head.slow == 2) {
-    pick_candidates<true>(p, r, rules, ws, splits, un.pick);
-    return;
-  }
   if (head.slow == 0) {
     if (rules.mode != Mode::Full) return;
     if (head.top <= kKeyNegInf) {
@@ -1346,8 +1231,8 @@ __device__ __forceinline__ void finish_one(const SampleParams& p, int row0, int 
     int n_cut = head.n_cut, n_pick = head.n_pick;
     if constexpr (kList) {
       const Grid grid{kPerNat / static_cast<double>(rules.tau)};
-      for (int s = 0; s * kBlockThreads < splits * kScanThreads; ++s) {
-        Pieces<kBf16, NV, kBlockThreads> z;
+      for (int s = 0; s < splits; ++s) {
+        Pieces<kBf16, NV, kScanThreads> z;
         z.load(p, r, s);
         __syncthreads();
         list_tokens(z, grid, in, counts);
@@ -1356,23 +1241,12 @@ __device__ __forceinline__ void finish_one(const SampleParams& p, int row0, int 
       n_cut = __hip_atomic_load(&in.n_cut, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       n_pick = __hip_atomic_load(&in.n_pick, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    if (n_cut <= kWaveList && n_pick <= kWaveList) {
-      if (wave_id() == 0) finish_row<false>(p, r, rules, in, head, n_cut, n_pick, un.pick);
-      return;
-    }
     if (n_cut <= kListCap && n_pick <= kListCap) {
-      finish_row<true>(p, r, rules, in, head, n_cut, n_pick, un.pick);
+      finish_row(p, r, rules, in, head, n_cut, n_pick, un.fin);
       return;
     }
   }
   sample_row<kBf16>(p, r, rules, un.row);
-}
-
-template <bool kBf16, int NV, bool kList>
-__global__ __launch_bounds__(kRowThreads) void sample_finish_kernel(SampleParams p, int row0, int splits) {
-  __shared__ FinishShared un;
-  __shared__ FilterCounts counts;
-  finish_one<kBf16, NV, kList>(p, row0, blockIdx.x, splits, un, counts);
 }
 
 // 16-byte pieces per thread: 32 tokens' worth, or fewer while that spreads a row over more
@@ -1402,12 +1276,12 @@ hipError_t launch_sample_nv(const SampleParams& p, int splits, hipStream_t strea
   for (int row0 = 0; row0 < p.R; row0 += kRowsPerLaunch) {
     const int rows = p.R - row0 < kRowsPerLaunch ? p.R - row0 : kRowsPerLaunch;
     sample_scan_kernel<kBf16, NV><<<rows * splits, kScanThreads, 0, stream>>>(p, row0, splits);
-    sample_place_kernel<<<rows, kFilterThreads, 0, stream>>>(p, row0, splits);
+    sample_place_kernel<<<rows, kPlaceThreads, 0, stream>>>(p, row0, splits);
     if (p.top_k) {
       sample_finish_kernel<kBf16, NV, true><<<rows, kRowThreads, 0, stream>>>(p, row0, splits);
     } else {
       sample_filter_kernel<kBf16, NV>
-          <<<rows * splits * (kScanThreads / kFilterThreads), kFilterThreads, 0, stream>>>(p, row0, rows, splits);
+          <<<rows * splits * (kScanThreads / kPlaceThreads), kPlaceThreads, 0, stream>>>(p, row0, rows, splits);
       sample_finish_kernel<kBf16, NV, false><<<rows, kRowThreads, 0, stream>>>(p, row0, splits);
     }
     const hipError_t e = hipGetLastError();
