@@ -647,7 +647,7 @@ struct PlaceShared {
   double part[kPlaceThreads / kWave];
   double value;
   unsigned long long most;
-  int counts[2 * kPlaceThreads / kWave];
+  int4 counts[2 * kPlaceThreads / kWave];
   int offset[kMaxSplits + 1];  // candidates in front of each split's
   int n, at;
 };
@@ -682,16 +682,33 @@ __device__ __forceinline__ unsigned long long candidate(const RowView& ws, const
   return ws.split[s].data[i - offset[s]];
 }
 
+// bisect() with three cuts a round, whose counts come back together: a round is a barrier and a
+// trip through LDS, whatever it counts.
+template <class T, class Count>
+__device__ __forceinline__ T quarter(T lo, T hi, int need, Count count) {
+  while (lo < hi) {
+    const T span = hi - lo, c1 = lo + span / 4 + 1, c2 = max(c1, lo + span / 2 + 1), c3 = max(c2, hi - span / 4);
+    const int4 c = count(c1, c2, c3);
+    if (c.z >= need) lo = c3;
+    else if (c.y >= need) lo = c2, hi = c3 - 1;
+    else if (c.x >= need) lo = c1, hi = c2 - 1;
+    else hi = c1 - 1;
+    if (c.x == need || c.y == need || c.z == need) return c.z == need ? c3 : c.y == need ? c2 : c1;
+  }
+  return lo;
+}
+
 // The cut that leaves exactly k of the candidates; at least k have a key >= least.  Keys of
 // bf16 logits differ in their upper half only (below it zeros, or ones if negative).
 template <class CountKeys, class CountTokens>
 __device__ __forceinline__ unsigned long long cut_to(const SampleParams& p, int k, uint32_t least, uint32_t top,
                                                      CountKeys keys, CountTokens tokens) {
   const int shift = p.is_bf16 ? 16 : 0;
-  uint32_t key = bisect<uint32_t>(least >> shift, top >> shift, k, k, [&](uint32_t m) { return keys(m << shift); })
+  uint32_t key = quarter<uint32_t>(least >> shift, top >> shift, k,
+                                   [&](uint32_t a, uint32_t b, uint32_t c) { return keys(a << shift, b << shift, c << shift); })
                  << shift;
   if (p.is_bf16 && !(key & 0x80000000u)) key |= 0xffffu;
-  return bisect<unsigned long long>(token_order(key, p.V - 1), token_order(key, 0), k, k, tokens);
+  return quarter<unsigned long long>(token_order(key, p.V - 1), token_order(key, 0), k, tokens);
 }
 
 // sh.token[0, n) in descending order (n <= kGridBins)
@@ -771,11 +788,16 @@ __device__ __forceinline__ bool pick_candidates(const SampleParams& p, int r, co
     least += static_cast<uint32_t>(kGridBins - 1 - first_bin(hit, kGridBins - 1, sh)) << shift;
   }
   __syncthreads();
-  for (int i = tid; i < n; i += kPlaceThreads) {
-    const unsigned long long v = candidate(ws, sh.offset, i);
-    if (order_key(v) < least) continue;
-    const int at = atomicAdd(&sh.n, 1);
-    if (at < kNearMax) sh.near[at] = v;
+  for (int i0 = tid; i0 < n; i0 += 4 * kPlaceThreads) {
+    unsigned long long v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = i0 + u * kPlaceThreads < n ? candidate(ws, sh.offset, i0 + u * kPlaceThreads) : 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (v[u] == 0 || order_key(v[u]) < least) continue;
+      const int at = atomicAdd(&sh.n, 1);
+      if (at < kNearMax) sh.near[at] = v[u];
+    }
   }
   __syncthreads();
   const int m = sh.n;
@@ -787,21 +809,32 @@ __device__ __forceinline__ bool pick_candidates(const SampleParams& p, int r, co
   unsigned long long cut = 1;
   if (m > k) {
     int turn = 0;
+    auto counts = [&](auto value, auto a, auto b, auto c) {
+      int4 n3 = make_int4(0, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        if (i * kPlaceThreads >= m) continue;
+        n3.x += popc64(__ballot(value(mine[i]) >= a));
+        n3.y += popc64(__ballot(value(mine[i]) >= b));
+        n3.z += popc64(__ballot(value(mine[i]) >= c));
+      }
+      int4* half = sh.counts + (turn++ & 1) * (kPlaceThreads / kWave);
+      if (lane == 0) half[wave_id()] = n3;
+      __syncthreads();
+      n3 = half[0];
+#pragma unroll
+      for (int w = 1; w < kPlaceThreads / kWave; ++w) {
+        n3.x += half[w].x;
+        n3.y += half[w].y;
+        n3.z += half[w].z;
+      }
+      return n3;
+    };
     cut = cut_to(
         p, k, least, top,
-        [&](uint32_t key) {
-          int c = 0;
-#pragma unroll
-          for (int i = 0; i < kMine; ++i)
-            if (i * kPlaceThreads < m) c += popc64(__ballot(order_key(mine[i]) >= key));
-          return block_count<kPlaceThreads>(c, sh.counts, turn++);
-        },
-        [&](unsigned long long token) {
-          int c = 0;
-#pragma unroll
-          for (int i = 0; i < kMine; ++i)
-            if (i * kPlaceThreads < m) c += popc64(__ballot(mine[i] >= token));
-          return block_count<kPlaceThreads>(c, sh.counts, turn++);
+        [&](uint32_t a, uint32_t b, uint32_t c) { return counts([](unsigned long long v) { return order_key(v); }, a, b, c); },
+        [&](unsigned long long a, unsigned long long b, unsigned long long c) {
+          return counts([](unsigned long long v) { return v; }, a, b, c);
         });
   }
   __syncthreads();

@@ -624,13 +624,13 @@ def accept(token: torch.Tensor, parent: torch.Tensor, target: torch.Tensor, tree
         raise ValueError("accept: token, parent and target must have the same length")
     _here(token, parent, target)
     offs_np, offs_ptr, B = _offsets(tree_offsets)  # offs_np: alive until the call returns
-    longest = T if offs_np is None else max(int(np.diff(offs_np).max(initial=0)), 0)
+    longest = T if offs_np is None else int((offs_np[1:] - offs_np[:-1]).max()) if B > 0 else 0
     if outputs is None:
-        dev = token.device
-        outputs = {"on_path": torch.empty(T, dtype=torch.uint8, device=dev),
-                   "path": torch.empty((B, longest), dtype=torch.int32, device=dev),
-                   "length": torch.empty(B, dtype=torch.int32, device=dev),
-                   "bonus": torch.empty(B, dtype=torch.int32, device=dev)}
+        # one allocation for the three int32 outputs
+        both = torch.empty(B * (max(longest, 0) + 2), dtype=torch.int32, device=token.device)
+        path, length, bonus = both.split((B * max(longest, 0), B, B))
+        outputs = {"on_path": torch.empty(T, dtype=torch.uint8, device=token.device),
+                   "path": path.view(B, max(longest, 0)), "length": length, "bonus": bonus}
     else:
         for name, dt, shape in (("on_path", torch.uint8, (T,)), ("length", torch.int32, (B,)),
                                 ("bonus", torch.int32, (B,))):
