@@ -764,16 +764,30 @@ __device__ __forceinline__ bool pick_candidates(const SampleParams& p, int r, co
     if (lane < splits) sh.offset[lane + 1] = upto;
     if (lane == 0) sh.offset[0] = sh.n = 0;
   }
+  // all candidates, eight of a thread's requested at a time
+  auto each_candidate = [&](auto take) {
+    constexpr int kLoads = 8;
+    for (int i0 = tid; i0 < n; i0 += kLoads * kPlaceThreads) {
+      unsigned long long v[kLoads];
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        const int i = i0 + u * kPlaceThreads;
+        v[u] = i < n ? candidate(ws, sh.offset, i) : 0;
+      }
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u)
+        if (v[u] != 0) take(v[u]);
+    }
+  };
   if (n > kNearMax) {
     // raise that bound: counts of 1024 equal ranges of keys
     int* count = reinterpret_cast<int*>(sh.sum);
     for (int i = tid; i < kGridBins; i += kPlaceThreads) count[i] = 0;
     __syncthreads();
     const int shift = max(0, 32 - __clz(static_cast<int>(top - least)) - 10);
-    for (int i = tid; i < n; i += kPlaceThreads) {
-      const uint32_t key = order_key(candidate(ws, sh.offset, i));
-      if (key >= least) atomicAdd(&count[(key - least) >> shift], 1);
-    }
+    each_candidate([&](unsigned long long v) {
+      if (order_key(v) >= least) atomicAdd(&count[(order_key(v) - least) >> shift], 1);
+    });
     __syncthreads();
     int mine = 0, incl[kPlaceMine];
 #pragma unroll
@@ -788,17 +802,11 @@ __device__ __forceinline__ bool pick_candidates(const SampleParams& p, int r, co
     least += static_cast<uint32_t>(kGridBins - 1 - first_bin(hit, kGridBins - 1, sh)) << shift;
   }
   __syncthreads();
-  for (int i0 = tid; i0 < n; i0 += 4 * kPlaceThreads) {
-    unsigned long long v[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) v[u] = i0 + u * kPlaceThreads < n ? candidate(ws, sh.offset, i0 + u * kPlaceThreads) : 0;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (v[u] == 0 || order_key(v[u]) < least) continue;
-      const int at = atomicAdd(&sh.n, 1);
-      if (at < kNearMax) sh.near[at] = v[u];
-    }
-  }
+  each_candidate([&](unsigned long long v) {
+    if (order_key(v) < least) return;
+    const int at = atomicAdd(&sh.n, 1);
+    if (at < kNearMax) sh.near[at] = v;
+  });
   __syncthreads();
   const int m = sh.n;
   if (m > kNearMax) return false;
