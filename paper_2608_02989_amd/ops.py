@@ -61,6 +61,14 @@ def _need(t: torch.Tensor, name: str, dtype=None, dim=None):
         raise ValueError(f"{name} must have {dim} dims")
 
 
+def _alloc(stream, make):
+    """make() with its tensors belonging to the stream that uses them."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        return make()
+
+
 def _here(t: torch.Tensor, *others):
     """All given tensors on the current device: launches go to its streams."""
     d = torch._C._cuda_getDevice()
@@ -259,8 +267,8 @@ def quantize_q4(w: torch.Tensor, stream=None) -> tuple[torch.Tensor, torch.Tenso
         raise ValueError(f"quantize_q4: the last dimension must be a multiple of {Q4_GROUP}, got {tuple(w.shape)}")
     _here(w)
     K = w.shape[-1]
-    codes = torch.empty((*w.shape[:-1], K // 2), dtype=torch.uint8, device=w.device)
-    scales = torch.empty((*w.shape[:-1], K // Q4_GROUP), dtype=torch.uint8, device=w.device)
+    codes, scales = _alloc(stream, lambda: tuple(
+        torch.empty((*w.shape[:-1], K // n), dtype=torch.uint8, device=w.device) for n in (2, Q4_GROUP)))
     check(lib().acceptmoe_quantize_q4(_ptr(w), _dtype_code(w), w.numel(), _ptr(codes), _ptr(scales), _stream_ptr(stream)))
     return codes, scales
 
@@ -293,7 +301,7 @@ def pack_gate_up_q4(gate: torch.Tensor, gate_scale: torch.Tensor, up: torch.Tens
     n = int(lib().acceptmoe_q4_gate_up_bytes(E, I, H))
     if n == 0:
         raise ValueError(f"unsupported gate/up shape E={E} I={I} H={H}")
-    data = torch.empty(n, dtype=torch.uint8, device=gate.device)
+    data = _alloc(stream, lambda: torch.empty(n, dtype=torch.uint8, device=gate.device))
     check(lib().acceptmoe_pack_gate_up_q4(_ptr(gate), _ptr(gate_scale), _ptr(up), _ptr(up_scale), E, I, H, _ptr(data),
                                           _stream_ptr(stream)))
     return PackedQ4(data, "gate_up", E, I, H)
@@ -305,7 +313,7 @@ def pack_down_q4(down: torch.Tensor, down_scale: torch.Tensor, stream=None) -> P
     n = int(lib().acceptmoe_q4_down_bytes(E, H, I))
     if n == 0:
         raise ValueError(f"unsupported down shape E={E} H={H} I={I}")
-    data = torch.empty(n, dtype=torch.uint8, device=down.device)
+    data = _alloc(stream, lambda: torch.empty(n, dtype=torch.uint8, device=down.device))
     check(lib().acceptmoe_pack_down_q4(_ptr(down), _ptr(down_scale), E, H, I, _ptr(data), _stream_ptr(stream)))
     return PackedQ4(data, "down", E, H, I)
 
@@ -341,13 +349,13 @@ def moe_forward_q4(hidden: torch.Tensor, w_gate_up: PackedQ4, w_down: PackedQ4, 
         raise ValueError("topk_idx / topk_gate must be [T, k]")
     _here(hidden, w_gate_up.data, w_down.data, topk_idx, topk_gate, out, workspace)
     if out is None:
-        out = torch.empty((T, H), dtype=torch.float32, device=hidden.device)
+        out = _alloc(stream, lambda: torch.empty((T, H), dtype=torch.float32, device=hidden.device))
     else:
         _need(out, "out", torch.float32, 2)
         if out.shape != hidden.shape:
             raise ValueError("out must be [T, H]")
     if workspace is None:
-        workspace = forward_q4_workspace(T, H, I, E, k, hidden.device)
+        workspace = _alloc(stream, lambda: forward_q4_workspace(T, H, I, E, k, hidden.device))
     check(lib().acceptmoe_moe_forward_q4(
         hidden.data_ptr(), w_gate_up.data.data_ptr(), w_down.data.data_ptr(), T, H, I, E, k, topk_idx.data_ptr(),
         topk_gate.data_ptr(), out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
@@ -531,13 +539,16 @@ def residual_norm(hidden: torch.Tensor, y: torch.Tensor | None, weight: torch.Te
         raise ValueError(f"residual_norm: H={H} is no multiple of the group {g}")
     _here(hidden, y, weight)
     if out is None:
-        dev = hidden.device
-        res = {"hidden": hidden if y is None else torch.empty_like(hidden)}
-        if g == 0:
-            res["norm"] = torch.empty_like(hidden)
-        else:
-            res["codes"] = torch.empty((T, H), dtype=torch.float8_e4m3fn, device=dev)
-            res["scale"] = torch.empty((T, 1 if g < 0 else H // g), dtype=torch.float32, device=dev)
+        def make():
+            res = {"hidden": hidden if y is None else torch.empty_like(hidden)}
+            if g == 0:
+                res["norm"] = torch.empty_like(hidden)
+            else:
+                res["codes"] = torch.empty((T, H), dtype=torch.float8_e4m3fn, device=hidden.device)
+                res["scale"] = torch.empty((T, 1 if g < 0 else H // g), dtype=torch.float32, device=hidden.device)
+            return res
+
+        res = _alloc(stream, make)
     else:
         res = dict(out) if y is not None else {**out, "hidden": hidden}
         want = [("hidden", hidden.dtype, (T, H))] if y is not None else []
@@ -593,8 +604,8 @@ def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: torch.Tenso
     _here(logits, uniform, temperature, top_k, top_p, min_p, workspace)
     dev = logits.device
     if outputs is None:
-        outputs = {"token": torch.empty(R, dtype=torch.int32, device=dev),
-                   "prob": torch.empty(R, dtype=torch.float32, device=dev)}
+        outputs = _alloc(stream, lambda: {"token": torch.empty(R, dtype=torch.int32, device=dev),
+                                          "prob": torch.empty(R, dtype=torch.float32, device=dev)})
     else:
         for name, dt in (("token", torch.int32), ("prob", torch.float32)):
             _need(outputs[name], name, dt, 1)
@@ -602,7 +613,7 @@ def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: torch.Tenso
                 raise ValueError(f"{name} must have {R} elements")
             _here(outputs[name])
     if workspace is None:
-        workspace = sample_workspace(R, V, dev)
+        workspace = _alloc(stream, lambda: sample_workspace(R, V, dev))
     check(lib().acceptmoe_sample(logits.data_ptr(), code, step if R > 1 else V, R, V, uniform.data_ptr(),
                                  _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
                                  outputs["token"].data_ptr(), outputs["prob"].data_ptr(), workspace.data_ptr(),
@@ -632,12 +643,15 @@ def accept(token: torch.Tensor, parent: torch.Tensor, target: torch.Tensor, tree
     else:
         offs, offs_ptr, B = _offsets(tree_offsets)
         longest = T if offs is None else int((offs[1:] - offs[:-1]).max(initial=0))
+    if B < 0:
+        raise ValueError("accept: tree_offsets must hold B + 1 entries, got none")
     if outputs is None:
         # one allocation for the three int32 outputs
-        both = torch.empty(B * (max(longest, 0) + 2), dtype=torch.int32, device=token.device)
+        both, on_path = _alloc(stream, lambda: (
+            torch.empty(B * (max(longest, 0) + 2), dtype=torch.int32, device=token.device),
+            torch.empty(T, dtype=torch.uint8, device=token.device)))
         path, length, bonus = both.split((B * max(longest, 0), B, B))
-        outputs = {"on_path": torch.empty(T, dtype=torch.uint8, device=token.device),
-                   "path": path.view(B, max(longest, 0)), "length": length, "bonus": bonus}
+        outputs = {"on_path": on_path, "path": path.view(B, max(longest, 0)), "length": length, "bonus": bonus}
     else:
         for name, dt, shape in (("on_path", torch.uint8, (T,)), ("length", torch.int32, (B,)),
                                 ("bonus", torch.int32, (B,))):

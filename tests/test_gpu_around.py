@@ -17,7 +17,7 @@ def say(*a):
 
 
 def dev(a, dt=None):
-    t = torch.as_tensor(np.ascontiguousarray(a))
+    t = torch.from_numpy(np.array(a))
     return (t if dt is None else t.to(dt)).to(DEV)
 
 
@@ -226,6 +226,38 @@ def test_sample_far_from_zero(gpu):
         check_sample(z.astype(np.float32), rng.random(6), **rules)
 
 
+def test_sample_on_its_own_stream_and_in_a_graph(gpu):
+    rng = np.random.default_rng(12)
+    side = torch.cuda.Stream()
+    for R, V, rules in ((3, 5000, {"top_k": 30, "top_p": 0.9}), (3, 40000, {"top_p": 0.9}), (40, 9000, {"min_p": 0.02})):
+        zs = [dev(logits(rng, R, V)) for _ in range(2)]
+        u = dev(rng.random(R).astype(np.float32))
+        args = {n: torch.full((R,), v, dtype=torch.int32 if n == "top_k" else torch.float32, device=DEV)
+                for n, v in rules.items()}
+        eager = [ops.sample(z, u, **args) for z in zs]
+        eager = [(e["token"].cpu(), e["prob"].cpu()) for e in eager]
+        side.wait_stream(torch.cuda.current_stream())
+        got = [ops.sample(z, u, **args, stream=side) for z in zs for _ in range(3)]
+        side.synchronize()
+        for n, o in enumerate(got):
+            assert torch.equal(o["token"].cpu(), eager[n // 3][0]) and torch.equal(o["prob"].cpu(), eager[n // 3][1])
+        ws = ops.sample_workspace(R, V, DEV)
+        graphs = []
+        for z in zs:
+            torch.cuda.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                out = ops.sample(z, u, **args, workspace=ws)
+            graphs.append((g, out))
+        for rep in range(3):
+            for n in (0, 1):
+                graphs[n][0].replay()
+                torch.cuda.synchronize()
+                assert torch.equal(graphs[n][1]["token"].cpu(), eager[n][0]), (rep, n)
+                assert torch.equal(graphs[n][1]["prob"].cpu(), eager[n][1])
+            ops.sample(zs[0], u)
+
+
 def test_sample_borders_of_u_and_top_p(gpu):
     z = np.log(np.tile(np.float32([4, 2, 1, 1]), (4, 1)))
     z = np.concatenate([z, np.full((4, 300), -INF, np.float32)], axis=1)
@@ -294,3 +326,59 @@ def test_accept_malformed_parents(gpu):
     token = np.ones(13, int)
     target = np.ones(13, int)
     check_accept(token, parent, target, [0, 8, 13])
+
+
+def test_accept_ways_to_give_trees(gpu):
+    rng = np.random.default_rng(7)
+    a, b = tree(rng, 5, 3, 0.6), tree(rng, 9, 3, 0.6)
+    parent, token, target = (np.concatenate([x, y]).astype(int) for x, y in zip(a, b))
+    parent[6:] += 5
+    for offs in ([0, 5, 5, 14], (0, 5, 5, 14), np.array([0, 5, 5, 14]), np.array([0, 5, 5, 14], np.int32),
+                 list(np.array([0, 5, 5, 14]))):
+        check_accept(token, parent, target, offs)
+    none = torch.zeros(0, dtype=torch.int32, device=DEV)
+    got = ops.accept(none, none, none, [0])
+    assert got["path"].shape == (0, 0) and got["length"].shape == (0,)
+
+
+def test_refusals(gpu):
+    """Arguments that do not fit together: an exception before any launch."""
+    h, y, w = (torch.zeros(s, device=DEV) for s in ((4, 64), (4, 64), (64,)))
+    ops.residual_norm(h, y, w)
+    for args, kw, err in (((h.half(), y, w.half()), {}, TypeError), ((h, y.bfloat16(), w), {}, TypeError),
+                          ((h, y, w.bfloat16()), {}, TypeError), ((h, y, w[:60]), {}, ValueError),
+                          ((h, y[:3], w), {}, ValueError), ((h.t(), y, w), {}, ValueError),
+                          ((h, y, w), {"group": 48}, ValueError), ((h, y, w), {"group": 128}, ValueError),
+                          ((h.cpu(), y, w), {}, ValueError), ((h, y, w), {"eps": -1.0}, ops.AcceptMoEError),
+                          ((h, y, w), {"out": {"hidden": h, "norm": y}}, ops.AcceptMoEError),
+                          ((h, y, w), {"out": {"hidden": y, "norm": h.clone()}}, ops.AcceptMoEError),
+                          ((h, y, w), {"out": {"hidden": h, "norm": h[:3].clone()}}, ValueError),
+                          ((h[:, :62].contiguous(), None, w[:62]), {}, ops.AcceptMoEError)):
+        with pytest.raises(err):
+            ops.residual_norm(*args, **kw)
+    z, u = torch.zeros(3, 40, device=DEV), torch.zeros(3, device=DEV)
+    f, i = torch.ones(3, device=DEV), torch.ones(3, dtype=torch.int32, device=DEV)
+    ops.sample(z, u)
+    for args, kw, err in (((z.half(), u), {}, TypeError), ((z[0], u), {}, ValueError), ((z, u[:2]), {}, ValueError),
+                          ((z, u.double()), {}, TypeError), ((z.t(), f), {}, ValueError), ((z.cpu(), u), {}, ValueError),
+                          ((z, u), {"top_k": f}, TypeError), ((z, u), {"top_p": f[:2]}, ValueError),
+                          ((z, u), {"temperature": i}, TypeError),
+                          ((z[:1].expand(3, 40), u), {}, ValueError),
+                          ((z, u), {"outputs": {"token": i, "prob": f[:2]}}, ValueError),
+                          ((z, u), {"workspace": torch.empty(256, dtype=torch.uint8, device=DEV)}, ops.AcceptMoEError),
+                          ((z[:, :0], u), {}, ops.AcceptMoEError)):
+        with pytest.raises(err):
+            ops.sample(*args, **kw)
+    t = torch.zeros(6, dtype=torch.int32, device=DEV)
+    ops.accept(t, t, t)
+    for args, kw, err in (((t.long(), t, t), {}, TypeError), ((t, t[:5], t), {}, ValueError),
+                          ((t, t, t, []), {}, ValueError), ((t, t, t, [0.0, 6.0]), {}, TypeError),
+                          ((t, t, t, [0, 5]), {}, ops.AcceptMoEError), ((t, t, t, [0, 4, 3, 6]), {}, ops.AcceptMoEError),
+                          ((t.cpu(), t, t), {}, ValueError)):
+        with pytest.raises(err):
+            ops.accept(*args, **kw)
+    out = ops.accept(t, t, t)
+    for name, bad in (("path", out["path"][:, :5].contiguous()), ("on_path", out["on_path"][:5]),
+                      ("length", out["length"].float())):
+        with pytest.raises((ValueError, TypeError)):
+            ops.accept(t, t, t, outputs={**out, name: bad})

@@ -112,6 +112,45 @@ def test_forward_at_layer_width(gpu, T):
     run_check(T, 2048, 768, 16, 8)
 
 
+@pytest.mark.parametrize("T,H,I,E,k", [(2100, 32, 32, 8, 8), (600, 32, 32, 40, 32), (5500, 32, 32, 3, 3),
+                                       (32, 64, 64, 64, 1), (4, 2048, 64, 512, 8), (16, 96, 32, 5, 2)])
+def test_forward_long_lists(gpu, T, H, I, E, k):
+    """More routing entries than the dispatch holds at a time; the largest blocks that need no dispatch."""
+    run_check(T, H, I, E, k)
+
+
+def test_forward_on_its_own_stream_and_in_a_graph(gpu):
+    """Calls on a side stream with tensors of their own, and two captured graphs that share a
+    workspace, replayed in turn with eager work between."""
+    for T, H, I, E, k in ((1, 256, 96, 8, 2), (40, 256, 96, 8, 2), (300, 256, 96, 8, 2)):
+        stacks, x, idx, g = case(T, T, H, I, E, k)
+        wgu, wd = packed(stacks)
+        xs = [x.to(DEV), (x * 0.5).to(DEV)]
+        i, gd = dev(idx), dev(g)
+        eager = [ops.moe_forward_q4(v, wgu, wd, i, gd).cpu() for v in xs]
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        got = [ops.moe_forward_q4(v, wgu, wd, i, gd, stream=side) for v in xs for _ in range(3)]
+        side.synchronize()
+        for n, y in enumerate(got):
+            assert torch.equal(y.cpu(), eager[n // 3])
+        ws = ops.forward_q4_workspace(T, H, I, E, k, DEV)
+        outs = [torch.empty(T, H, device=DEV) for _ in xs]
+        graphs = []
+        for v, o in zip(xs, outs):
+            torch.cuda.synchronize()
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1], stream=side):
+                ops.moe_forward_q4(v, wgu, wd, i, gd, out=o, workspace=ws)
+        for rep in range(3):
+            for n in (0, 1):
+                outs[n].fill_(float("nan"))
+                graphs[n].replay()
+                torch.cuda.synchronize()
+                assert torch.equal(outs[n].cpu(), eager[n]), (T, rep, n)
+            ops.moe_forward_q4(xs[0], wgu, wd, i, gd)
+
+
 def test_forward_scales_across_the_range(gpu):
     """Scale bytes from 2 to 252 in one stack: weights from 2^-126 to 6 * 2^125, each row's
     output compared with what its own magnitude allows."""
