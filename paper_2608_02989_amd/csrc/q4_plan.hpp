@@ -15,11 +15,12 @@ constexpr int q4_gate_up_quads(int I) { return (I + 31) / 32; }
 constexpr int q4_down_quads(int H) { return (H + 63) / 64; }
 constexpr size_t q4_quad_run(int K) { return static_cast<size_t>(q4_chunks(K)) * kQ4QuadBytes; }
 
-// Most rows of an item.  Blocks of up to kQ4SmallT tokens, with few items for the device's
-// CUs, take items of 32 rows and workgroups of two waves (64 tokens in 26 experts, H = 4096,
-// I = 1536: 312 workgroups of four waves on 256 CUs took as long as 512).
-constexpr int kQ4SmallT = 256;
-constexpr int q4_item_limit(int T) { return T <= kQ4SmallT ? 32 : 64; }
+// Most rows of an item: fewer for smaller blocks, whose items are few for 256 CUs, while an expert's
+// second item reads its weights again, mostly from L2.  H = 2048, I = 768, top-8 in us with 32 /
+// 48 / 64 rows: 320 tokens in 40 experts 63 / 67 / 71, 512 in 64 88 / 84 / 93, 1024 in 128 157 /
+// 154 / 163, 1920 in 128 245 / 249 / 239.
+constexpr int q4_item_limit(int T, int k) { return T * k <= 2560 ? 32 : T * k <= 8192 ? 48 : 64; }
+constexpr int kQ4LeastLimit = 32;
 
 // An expert's `count` rows in equal runs of whole M-tiles, at most `limit` each.
 constexpr int q4_item_rows(int count, int limit) {
@@ -30,11 +31,14 @@ constexpr int q4_items(int count, int limit) {
   return (count + q4_item_rows(count, limit) - 1) / q4_item_rows(count, limit);
 }
 
-// Blocks of up to this many routing entries (and 16 tokens) take two launches without a
-// dispatch: every workgroup finds its expert in the entries itself.
+// Blocks of up to kQ4FewSlots routing entries take two launches without a dispatch: every
+// workgroup finds its expert in the entries itself.  The second one reads a row of activations
+// per expert and token, kQ4FewRows at most.  128 experts, H = 2048, I = 768, in us, so and by
+// dispatch: 1 token top-8 9.9 / 24.7, 2 top-8 16.5 / 25.5, 3 top-8 24.6 / 31, 4 top-8 32 / 29,
+// 16 top-1 25 / 23; H = 4096, I = 1536: 1 top-8 26 / 43, 2 top-8 47 / 44.
 constexpr int kQ4FewSlots = 32;
-constexpr int kQ4FewT = 16;
-constexpr bool q4_few(int T, int k) { return T <= kQ4FewT && T * k <= kQ4FewSlots; }
+constexpr int kQ4FewRows = 96;
+constexpr bool q4_few(int T, int k) { return T <= 16 && T * k <= kQ4FewSlots && T * T * k <= kQ4FewRows; }
 
 // most items of a block of `slots` routing entries: one per active expert and one
 // more per full item
