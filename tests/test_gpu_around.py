@@ -86,6 +86,22 @@ def test_residual_norm(gpu, T, H, dtype, group, add):
     assert (np.abs(code - want) <= np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** -10) + near * (1 + 2.0 ** -4)).all()
 
 
+def test_residual_norm_beyond_32_bits(gpu):
+    """More than 2^31 elements: the last rows as in a call of their own."""
+    T, H = 525000, 4096
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    h = torch.zeros(T, H, dtype=torch.bfloat16, device=DEV)
+    y = torch.zeros(T, H, device=DEV)
+    h[-3:], y[-3:] = torch.randn(3, H, generator=gen, device=DEV).bfloat16(), torch.randn(3, H, generator=gen, device=DEV)
+    w = torch.rand(H, generator=gen, device=DEV).bfloat16()
+    for group in (None, 128):
+        want = ops.residual_norm(h[-3:].clone(), y[-3:].clone(), w, group=group)
+        got = ops.residual_norm(h, y, w, group=group)
+        for name in want:
+            assert torch.equal(got[name][-3:].view(torch.uint8), want[name].view(torch.uint8)), name
+        del got
+
+
 def test_residual_norm_zero_rows_and_in_place(gpu):
     h = torch.zeros(3, 64, dtype=torch.bfloat16)
     h[1] = 2.0
@@ -256,6 +272,38 @@ def test_sample_on_its_own_stream_and_in_a_graph(gpu):
                 assert torch.equal(graphs[n][1]["token"].cpu(), eager[n][0]), (rep, n)
                 assert torch.equal(graphs[n][1]["prob"].cpu(), eager[n][1])
             ops.sample(zs[0], u)
+
+
+def test_sample_rows_beyond_32_bits(gpu):
+    """Rows 2^31 elements apart."""
+    V, step = 5000, 2 ** 31
+    z = dev(logits(np.random.default_rng(8), 3, V), torch.bfloat16)
+    big = torch.empty(2 * step + V, dtype=torch.bfloat16, device=DEV).as_strided((3, V), (step, 1))
+    big.copy_(z)
+    u = torch.tensor([0.2, 0.5, 0.9], device=DEV)
+    for k in (None, torch.full((3,), 40, dtype=torch.int32, device=DEV)):
+        a, b = ops.sample(z, u, top_k=k), ops.sample(big, u, top_k=k)
+        assert torch.equal(a["token"], b["token"]) and torch.equal(a["prob"], b["prob"])
+
+
+def test_sample_settings_at_the_ends_of_their_types(gpu):
+    """Every row gets one of its tokens, whatever its settings hold."""
+    tiny, nan = float(np.finfo(np.float32).smallest_subnormal), float("nan")
+    rows = [(t, p, m, k, u) for t in (1.0, tiny, 3e38, INF, nan, -INF) for p in (1.0, 0.5, nan, -INF, INF, tiny)
+            for m in (0.0, 0.5, nan, INF, -INF) for k in (0, 3, -2 ** 31, 2 ** 31 - 1) for u in (0.0, 0.7, nan, INF, -1.0)]
+    t, p, m, k, u = (dev(np.array(c, np.int32 if i == 3 else np.float32)) for i, c in enumerate(zip(*rows)))
+    rng = np.random.default_rng(4)
+    for V in (70, 6000):
+        z = logits(rng, len(rows), V).astype(np.float32)
+        z[::3, 5:60] = -INF
+        z[1::7, 9] = INF
+        z[2::5, 11] = nan
+        for args in ({"top_k": k}, {}):
+            out = ops.sample(dev(z), u, temperature=t, top_p=p, min_p=m, **args)
+            token, prob = out["token"].cpu().numpy(), out["prob"].cpu().numpy()
+            assert ((token >= 0) & (token < V)).all()
+            chosen = z[np.arange(len(rows)), token]
+            assert (chosen > -INF).all() and ((prob > 0) & (prob <= 1)).all()
 
 
 def test_sample_borders_of_u_and_top_p(gpu):
