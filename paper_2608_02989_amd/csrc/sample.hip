@@ -17,8 +17,8 @@
 // 35.5 us of the call's 60, 2.9 TB/s, vector instructions per logit); with few the
 // latency of three or four launches of short dependent steps (one row of 32000: 6.8 us
 // for the pass, 10 for cutting and ordering its top 64, 2.4 for the launch that has
-// nothing left to do; 64 fp32 rows of 131072 with top-p alone: 14.5, 10.4, then 14.2 for the
-// second pass and 17.8 for the order within two bins).
+// nothing left to do; 64 fp32 rows of 131072 with top-p alone: 14.5, 10.4, then 14.1 for the
+// second pass and 13.3 for the order within two bins).
 #include "common.hpp"
 #include "launch.hpp"
 
@@ -632,16 +632,6 @@ __device__ __forceinline__ unsigned long long wave_sum_u64(unsigned long long v)
   return static_cast<unsigned long long>(__double_as_longlong(dpp::reduce(__longlong_as_double(v), 0.0, add)));
 }
 
-// Sum of the weights of the tokens from `token` on (itself and all larger).
-__device__ __forceinline__ unsigned long long sum_through(const unsigned long long* tokens,
-                                                          const unsigned long long* weights, int n,
-                                                          unsigned long long token) {
-  unsigned long long s = 0;
-#pragma unroll 4
-  for (int j = 0; j < n; ++j) s += tokens[j] >= token ? weights[j] : 0;
-  return s;
-}
-
 constexpr int kPlaceThreads = 256;
 constexpr int kPlaceMine = kGridBins / kPlaceThreads;  // neighbouring bins (or sorted tokens) of a thread
 constexpr int kDirect = 128;
@@ -1095,14 +1085,14 @@ constexpr int kFinishMine = kListCap / kRowThreads;
 constexpr int kWindow = 64;  // tokens around a place, ordered by adding up all larger ones
 
 struct FinishShared {
-  unsigned long long token[kWindow], weight[kWindow];
-  double step[kGridBins];  // exp(-b / 32)
+  ulonglong2 near[kWindow];  // token and weight
+  double step[kGridBins];    // exp(-b / 32)
   unsigned long long part64[2 * kRowThreads / kWave];
   int part32[2 * kRowThreads / kWave];
   uint32_t range[2 * kRowThreads / kWave];
   unsigned long long found;
   double sum;
-  int n;
+  int n, hit;
 };
 
 union FinishUnion {
@@ -1180,29 +1170,46 @@ __device__ __forceinline__ PlaceInList place_in_list(const Listed& l, int t0, do
   __syncthreads();
   if (tid == 0) {
     sh.n = 0;
-    sh.found = ~0ull;
+    sh.hit = 0;
   }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kFinishMine; ++i) {
     if (l.token[i] == 0 || l.token[i] < lo || l.token[i] >= hi) continue;
     const int at = atomicAdd(&sh.n, 1);  // kWindow at most
-    sh.token[at] = l.token[i];
-    sh.weight[at] = l.weight[i];
+    sh.near[at] = make_ulonglong2(l.token[i], l.weight[i]);
   }
   __syncthreads();
-  const int m = sh.n;
-  if (tid < kWave) {
-    const unsigned long long v = lane < m ? sh.token[lane] : ~0ull, w = lane < m ? sh.weight[lane] : 0;
-    const unsigned long long s = above + (lane < m ? sum_through(sh.token, sh.weight, m, v) : 0);
-    const double sum = before + static_cast<double>(s) * unit;
-    const bool here = lane < m && passes(sum) && !passes(before + static_cast<double>(s - w) * unit);
-    if (lane < m && __ballot(here) == 0) atomicMin(&sh.found, v);  // none: the smallest
-    wave_lds_sync();
-    if (here || (lane < m && sh.found == v) || (m == 0 && lane == 0)) {
-      sh.found = m == 0 ? 0 : v;
-      sh.sum = m == 0 ? before : sum;
-    }
+  // the sum up to each token, by kShare threads (with one thread each the kernel took 17.8 us instead of 13.3)
+  constexpr int kShare = kRowThreads / kWindow;
+  const int m = sh.n, t = tid / kShare;
+  const unsigned long long v = t < m ? sh.near[t].x : ~0ull, w = t < m ? sh.near[t].y : 0;
+  unsigned long long s = 0;
+  int c = 0;
+#pragma unroll
+  for (int j = 0; j < kWindow / kShare; ++j) {
+    const int at = j * kShare + tid % kShare;
+    const ulonglong2 other = sh.near[at];
+    const bool up = at < m && other.x >= v;
+    s += up ? other.y : 0;
+    c += up ? 1 : 0;
+  }
+  for (int o = 1; o < kShare; o *= 2) {
+    s += __shfl_xor(s, o);
+    c += __shfl_xor(c, o);
+  }
+  s += above;
+  const double sum = before + static_cast<double>(s) * unit;
+  const bool mine = t < m && tid % kShare == 0;
+  if (mine && passes(sum) && !passes(before + static_cast<double>(s - w) * unit)) {
+    sh.hit = 1;
+    sh.found = v;
+    sh.sum = sum;
+  }
+  __syncthreads();
+  if (sh.hit == 0 && ((mine && c == m) || (m == 0 && tid == 0))) {  // none: the smallest
+    sh.found = m == 0 ? 0 : v;
+    sh.sum = m == 0 ? before : sum;
   }
   __syncthreads();
   return {sh.found, sh.sum};
@@ -1215,11 +1222,13 @@ __device__ __forceinline__ void finish_row(const SampleParams& p, int r, const R
                                            const RowHead& head, int n_cut, int n_pick, FinishShared& sh) {
   const int tid = threadIdx.x;
   const Grid grid{kPerNat / static_cast<double>(rules.tau)};
+#pragma unroll 1
   for (int b = tid; b < kGridBins; b += kRowThreads) sh.step[b] = exp(-b / kPerNat);
   __syncthreads();
   double total = head.total;
   unsigned long long token = 0;
   // first the list in which the kept prefix ends, then that in which the sample lies
+#pragma unroll 1
   for (int step = head.t_cut >= 0 ? 0 : 1; step < 2; ++step) {
     const unsigned long long* list = step == 0 ? in.cut : in.pick;
     const int t0 = step == 0 ? head.t_cut : head.t_pick0;
@@ -1278,7 +1287,7 @@ __device__ __forceinline__ void finish_row(const SampleParams& p, int r, const R
 // A row that is not done yet, by a workgroup.  kList: lists the bins' tokens itself, part after
 // part; used beside top_k, where few rows need it.
 template <bool kBf16, int NV, bool kList>
-__global__ __launch_bounds__(kRowThreads) void sample_finish_kernel(SampleParams p, int row0, int splits) {
+__global__ __launch_bounds__(kRowThreads) __attribute__((amdgpu_waves_per_eu(4))) void sample_finish_kernel(SampleParams p, int row0, int splits) {
   __shared__ FinishUnion un;
   __shared__ FilterCounts counts;
   const int local = blockIdx.x, r = row0 + local, tid = threadIdx.x;

@@ -647,11 +647,11 @@ def accept(token: torch.Tensor, parent: torch.Tensor, target: torch.Tensor, tree
         raise ValueError("accept: tree_offsets must hold B + 1 entries, got none")
     if outputs is None:
         # one allocation for the three int32 outputs
-        both, on_path = _alloc(stream, lambda: (
-            torch.empty(B * (max(longest, 0) + 2), dtype=torch.int32, device=token.device),
-            torch.empty(T, dtype=torch.uint8, device=token.device)))
-        path, length, bonus = both.split((B * max(longest, 0), B, B))
-        outputs = {"on_path": on_path, "path": path.view(B, max(longest, 0)), "length": length, "bonus": bonus}
+        longest = max(longest, 0)
+        both, on_path = _alloc(stream, lambda: (token.new_empty(B * (longest + 2)),
+                                                token.new_empty(T, dtype=torch.uint8)))
+        path, length, bonus = torch.unsafe_split_with_sizes(both, (B * longest, B, B))
+        outputs = {"on_path": on_path, "path": path.view(B, longest), "length": length, "bonus": bonus}
     else:
         for name, dt, shape in (("on_path", torch.uint8, (T,)), ("length", torch.int32, (B,)),
                                 ("bonus", torch.int32, (B,))):
