@@ -303,7 +303,7 @@ __device__ void sample_row(const SampleParams& p, int r, const Rules& rules, Row
 //   other top_k, more candidates or tokens in a bin than the lists hold (many
 //     equal logits): `finish` runs sample_row.
 // ---------------------------------------------------------------------------
-constexpr int kScanThreads = 512;   // four workgroups per CU, in different phases
+constexpr int kScanThreads = 512;
 constexpr int kCandCap = 1280;      // candidates of a split
 constexpr int kGridBins = 1024;     // 32 nats below the largest logit; weights beyond sum to less than 2^20 e^-31
 constexpr int kCopies = 4;          // of each bin, by lane, against LDS atomics on one address
@@ -452,8 +452,11 @@ __device__ __forceinline__ T bisect(T lo, T hi, int need, int enough, Count coun
   return lo;
 }
 
+// Six waves per SIMD: registers that hold all pieces, and three workgroups per CU (a call on 512
+// bf16 rows of 100003, top-100: 61.4 us; cut to eight, with registers spilled, 60.6, without a
+// bound 70.9; on 64 fp32 rows of 131072, top-64: 27.6, 31.4, 27.5).
 template <bool kBf16, int NV>
-__global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(8))) void sample_scan_kernel(
+__global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(6))) void sample_scan_kernel(
     SampleParams p, int row0, int splits) {
   __shared__ unsigned long long s_bin[kGridBins * kCopies];
   __shared__ uint32_t s_max[2 * kScanThreads / kWave];
@@ -493,7 +496,6 @@ __global__ __launch_bounds__(kScanThreads) __attribute__((amdgpu_waves_per_eu(8)
     const double grid_top = floor(grid.at(top));
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      __builtin_amdgcn_sched_barrier(0);  // piece after piece: interleaved they spill 59 registers
 #pragma unroll
       for (int j = 0; j < Pieces<kBf16, NV, kScanThreads>::kPer; ++j) {
         const double g = static_cast<double>(z.logit(i, j)) * grid.scale, b = floor(g);
