@@ -4,10 +4,10 @@
 //   out_t = sum_j g_{t,j} W_d (silu(W_g x_t) * W_u x_t)
 //
 // Bound: with few rows per expert the weights' bytes (64 tokens in 26 experts, H = 4096,
-// I = 1536: gate/up 174 MB in 39 us, 4.5 TB/s, down 87 MB in 27.5 us), with many the matrix cores
+// I = 1536: gate/up 174 MB in 39 us, 4.5 TB/s, down 87 MB in 27 us), with many the matrix cores
 // and the expansion of the codes in front of them (1920 tokens, top-8, H = 2048, I = 768: 97
-// and, with the second plane, 97 GFLOP in 128 us each, 760 TFLOP/s of the 1248 that a large
-// bf16 product reaches), for a few tokens latency (one token: 6.1 and 5.8 us).
+// and, with the second plane, 97 GFLOP in 108 to 128 us each, 760 to 890 TFLOP/s of the 1248 that a large
+// bf16 product reaches), for a few tokens latency (one token: 6.3 and 5.7 us).
 //
 // Both factors of the gate and up products are exact in bf16 (a code has 2
 // significant bits, its scale is a power of two), so they run on the bf16 MFMA

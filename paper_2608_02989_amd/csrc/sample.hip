@@ -14,11 +14,11 @@
 // not depend on the order of the additions.
 //
 // Bound: with many rows the first pass over the logits (512 rows of 100003 in bf16, 102 MB:
-// 35.5 us of the call's 60, 2.9 TB/s, vector instructions per logit); with few the
-// latency of three or four launches of short dependent steps (one row of 32000: 6.8 us
-// for the pass, 10 for cutting and ordering its top 64, 2.4 for the launch that has
-// nothing left to do; 64 fp32 rows of 131072 with top-p alone: 14.5, 10.4, then 14.1 for the
-// second pass and 13.3 for the order within two bins).
+// 35.5 us of the call's 58, 2.9 TB/s, vector instructions per logit); with few the
+// latency of three or four launches of short dependent steps (one row of 32000: 6.3 us
+// for the pass, 9.7 for cutting and ordering its top 64, 2.5 for the launch that has
+// nothing left to do; 64 fp32 rows of 131072 with top-p alone: 13.9, 10.5, then 13.5 for the
+// second pass and 13.7 for the order within two bins).
 #include "common.hpp"
 #include "launch.hpp"
 
@@ -122,7 +122,7 @@ __device__ __forceinline__ void block_range(uint32_t& high, uint32_t& low, uint3
 // ---------------------------------------------------------------------------
 // Any row, by one workgroup over the row in memory: a radix search by digits of 11,
 // 11 and 10 bits of the key, with the weights (or counts) of each digit summed
-// in LDS.  (For all rows: 148 / 647 / 1221 us where the spread form below takes 17 / 55 / 60.)
+// in LDS.  (For all rows: 148 / 647 / 1221 us where the spread form below takes 17 / 51 / 58.)
 // ---------------------------------------------------------------------------
 constexpr int kRowThreads = 512;
 constexpr int kDigit = 11;
