@@ -311,7 +311,8 @@ int32_t acceptmoe_moe_forward(const void* hidden, int32_t dtype, const void* w_g
  * acceptmoe_moe_forward_q4 -- acceptmoe_moe_forward over such weights: hidden
  * [T, H] bf16, the same routing, out [T, H] fp32.  The products of the gate and up
  * projections are exact with fp32 accumulation; the activation goes to the down
- * projection in 16 significant bits (as two bf16 numbers).  Deterministic.
+ * projection in 16 significant bits (as two bf16 numbers); an activation past
+ * bf16's largest number, or not finite, makes its token's outputs NaN.  Deterministic.
  *   H and I positive multiples of 32 up to 65536, 1 <= E <= ACCEPTMOE_MAX_EXPERTS,
  *   1 <= k <= ACCEPTMOE_MAX_TOPK, T * H < 2^31 - 8; T == 0 is a no-op.  workspace as for
  *   acceptmoe_moe_forward, of acceptmoe_moe_forward_q4_workspace_size bytes.
@@ -387,7 +388,7 @@ int32_t acceptmoe_residual_norm(const void* hidden, int32_t dtype, const float* 
  *                [0, 1 - 2^-24])
  *   temperature, top_p, min_p  [R] device fp32, or NULL: 1 / no filter
  *   top_k        [R] device int32, or NULL
- *   token, prob  [R] device int32 / fp32, written
+ *   token, prob  [R] device int32 / fp32, written; they overlap no other argument
  *   workspace    acceptmoe_sample_workspace_size(R, V) bytes, 256-byte aligned,
  *                not shared by calls that may run concurrently
  *   1 <= V <= ACCEPTMOE_MAX_VOCAB, R <= ACCEPTMOE_MAX_SAMPLE_ROWS; R == 0 is a no-op.
