@@ -151,6 +151,15 @@ def test_forward_on_its_own_stream_and_in_a_graph(gpu):
             ops.moe_forward_q4(xs[0], wgu, wd, i, gd)
 
 
+@pytest.mark.parametrize("T,H,I,E,k", [(4, 192, 160, 64, 6), (9, 192, 160, 64, 1), (10, 192, 160, 64, 1),
+                                       (2, 320, 96, 64, 16), (1, 2048, 768, 64, 32), (3, 96, 224, 40, 10),
+                                       (640, 160, 96, 8, 4), (641, 160, 96, 8, 4), (2048, 96, 64, 40, 4),
+                                       (2049, 96, 64, 40, 4), (700, 160, 192, 9, 4)])
+def test_forward_where_the_kernels_change(gpu, T, H, I, E, k):
+    """The last block without a dispatch and the first with one; items of 32, 48 and 64 rows."""
+    run_check(T, H, I, E, k)
+
+
 def test_forward_scales_across_the_range(gpu):
     """Scale bytes from 2 to 252 in one stack: weights from 2^-126 to 6 * 2^125, each row's
     output compared with what its own magnitude allows."""
@@ -318,3 +327,30 @@ def test_verification_pass(gpu):
             assert torch.equal(a.cpu(), b), rep
         whole()  # eager work between replays
         torch.cuda.synchronize()
+
+
+def test_stack_twin_and_refused_norms(gpu):
+    """Two blocks in flight on two streams give what each gives alone; norms that do not fit."""
+    cfg, made = small(2)
+    layers = [m[0] for m in made]
+    norms = [torch.full((cfg.H,), 0.5 + l, dtype=torch.bfloat16, device=DEV) for l in range(3)]
+    blocks = [W.make_block(cfg, block=b) for b in range(2)]
+    T = len(blocks[0].parent)
+    stack = ops.VerifyStack(layers, T, norms=norms)
+    args = [(torch.from_numpy(b.hidden).bfloat16().to(DEV), *(dev(a) for a in (b.parent, b.depth, b.prob)), b.offsets)
+            for b in blocks]
+    alone = [stack.step(*a).clone() for a in args]
+    twin, streams = stack.twin(), [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [s.step(*a, stream=st) for s, a, st in zip((stack, twin), args, streams)]
+    torch.cuda.synchronize()
+    for a, b in zip(alone, got):
+        assert torch.equal(a, b)
+    for bad, err in ((norms[:2], ValueError), ([n[:-1] for n in norms], ValueError), ([n.float() for n in norms], TypeError),
+                     ([n.cpu() for n in norms], ValueError)):
+        with pytest.raises(err):
+            ops.VerifyStack(layers, T, norms=bad)
+    with pytest.raises(ValueError):
+        layers[0].step(torch.zeros(2 * cfg.T + 1, cfg.H, dtype=torch.bfloat16, device=DEV), *args[0][1:4])
+    with pytest.raises(TypeError):
+        layers[0].step(args[0][0].float(), *args[0][1:4])
