@@ -375,7 +375,7 @@ int32_t acceptmoe_residual_norm(const void* hidden, int32_t dtype, const float* 
  * The filters keep a prefix of that order, one after the other:
  *   top_k   the first top_k tokens (<= 0: all)
  *   top_p   the shortest prefix with C_j >= top_p * C of what top_k left, at
- *           least one token (>= 1: all)
+ *           least one token (<= 0: the first alone; >= 1: all)
  *   min_p   of these the tokens with w_j >= min_p (<= 0: all; above 1 counts as 1)
  * token[r] is the first kept j with C_j > u C_kept, prob[r] = w_j / C_kept its
  * probability.  temperature <= 0 (or NaN): the largest logit's token (the lowest

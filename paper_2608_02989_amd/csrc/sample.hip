@@ -1115,14 +1115,17 @@ struct PlaceInList {
 };
 
 // The token of a list, from bin t0 on, at which passes(before + sum up to it) turns true, and that
-// sum; the list's last one if it never does.  The order is searched by halves until at most
-// kWindow tokens are left around the place.
+// sum; the list's last one if it never does, its first one where `before` passes by itself (a
+// border of 0, or one that a rounding puts in front of the list).  The order is searched by
+// halves until at most kWindow tokens are left around the place.
 template <class Passes>
 __device__ __forceinline__ PlaceInList place_in_list(const Listed& l, int t0, double before, FinishShared& sh,
                                                      Passes passes) {
   constexpr int kWaves = kRowThreads / kWave;
   const int tid = threadIdx.x, lane = lane_id();
   const double unit = sh.step[t0] / kWeightOne;
+  // an empty sum reaches nothing
+  auto reached = [&](unsigned long long sum) { return sum != 0 && passes(before + static_cast<double>(sum) * unit); };
   // every token lies in [lo, hi): a list's keys share their upper bits
   uint32_t least = ~0u, most = 0;
 #pragma unroll
@@ -1159,7 +1162,7 @@ __device__ __forceinline__ PlaceInList place_in_list(const Listed& l, int t0, do
       w += sh.part64[half + i];
       c += sh.part32[half + i];
     }
-    if (passes(before + static_cast<double>(w) * unit)) {
+    if (reached(w)) {
       lo = mid;
       inside = c - count_above;
     } else {
@@ -1203,7 +1206,7 @@ __device__ __forceinline__ PlaceInList place_in_list(const Listed& l, int t0, do
   s += above;
   const double sum = before + static_cast<double>(s) * unit;
   const bool mine = t < m && tid % kShare == 0;
-  if (mine && passes(sum) && !passes(before + static_cast<double>(s - w) * unit)) {
+  if (mine && reached(s) && !reached(s - w)) {
     sh.hit = 1;
     sh.found = v;
     sh.sum = sum;

@@ -320,6 +320,27 @@ def test_sample_borders_of_u_and_top_p(gpu):
     assert ops.sample(dev(z)[:0], u[:0])["token"].shape == (0,)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("top_k", [None, 0, 3, 2000, 6000])
+def test_sample_top_p_of_nothing_keeps_the_first_token(gpu, dtype, top_k):
+    """top_p of 0, below 0 and next to it on rows whose first tokens are equal or nearly so: fewer of them than a
+    search's window holds, more, and more than a list holds; every way a row can take."""
+    V = 6000
+    rng = np.random.default_rng(31)
+    z = np.tile((rng.standard_normal(V) - 9).astype(np.float32), (6, 1))
+    z[0, [4000, 17, 2500]] = 5.0, 5.0, 1.0
+    z[1, [4000, 17, 2500]] = 5.001, 5.0, 4.999
+    z[2, rng.permutation(V)[:300]] = 2.0
+    z[3, rng.permutation(V)[:300]] = 2.0 + 0.02 * rng.random(300)
+    z[4, rng.permutation(V)[:5000]] = -1.0
+    z[5, 1234] = 7.0
+    for temperature in (None, 50.0):
+        for p in (0.0, -1.0, -INF, float(np.finfo(np.float32).smallest_subnormal), 1e-30):
+            say("top_p", p, "top_k", top_k, dtype, temperature)
+            for u in (0.0, 0.5, 0.9, 1 - 2.0 ** -24):
+                check_sample(z, np.full(6, u), dtype, top_p=p, top_k=top_k, temperature=temperature)
+
+
 # ---------------------------------------------------------------------------
 # accepted path
 # ---------------------------------------------------------------------------
