@@ -362,7 +362,10 @@ int32_t acceptmoe_residual_add(const void* hidden, int32_t dtype, const float* y
  *   norm_out    must overlap no input; scale_out is unused when group == 0
  *   H % 4 == 0, H <= 65536, eps finite and >= 0; group 0, -1, 32, 64, 128 or 256
  *   and a divisor of H.  All pointers 16-byte aligned (scale_out: 4).
- * The sum of squares is held in fp32, in a fixed order (deterministic).
+ * The sum of squares is held in fp32, in a fixed order (deterministic).  Values that are
+ * not finite follow the formulas: a NaN in s makes its row NaN; an infinity leaves NaN in
+ * its place (in 8 bits in the codes and the scale of its group) and zeros in the rest;
+ * a row of zeros with eps == 0 is NaN (0 / 0).
  */
 int32_t acceptmoe_residual_norm(const void* hidden, int32_t dtype, const float* y, const void* weight, int32_t T,
                                 int32_t H, float eps, int32_t group, void* hidden_out, void* norm_out,

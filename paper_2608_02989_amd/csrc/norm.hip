@@ -20,10 +20,16 @@ constexpr float kE4m3Max = 448.f;
 
 enum class NormOut { Plain, Groups, Row };
 
-// sum (kMax: largest) over the workgroup's threads, in a fixed order
+// larger of two magnitudes; their bits are ordered like them, and a NaN's stand above all (fmaxf
+// would drop it, and a broken row would leave as codes and scales of a sound one)
+__device__ __forceinline__ float larger(float a, float b) {
+  return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
+}
+
+// sum (kMax: largest magnitude) over the workgroup's threads, in a fixed order
 template <bool kMax>
 __device__ __forceinline__ float block_reduce(float v, float* part) {
-  auto op = [](float a, float b) { return kMax ? fmaxf(a, b) : a + b; };
+  auto op = [](float a, float b) { return kMax ? larger(a, b) : a + b; };
   v = dpp::reduce(v, 0.f, op);
   const int waves = blockDim.x / kWave;
   if (waves == 1) return v;
@@ -103,11 +109,13 @@ __global__ __launch_bounds__(1024) void residual_norm_kernel(const void* __restr
       if (c < n4) store4(norm_out, row + c, s[i]);
     }
   } else {
-    auto largest = [&](int i) { return fmaxf(fmaxf(fabsf(s[i].x), fabsf(s[i].y)), fmaxf(fabsf(s[i].z), fabsf(s[i].w))); };
+    auto largest = [&](int i) {
+      return larger(larger(fabsf(s[i].x), fabsf(s[i].y)), larger(fabsf(s[i].z), fabsf(s[i].w)));
+    };
     float row_max = 0.f;
     if constexpr (kOut == NormOut::Row) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) row_max = fmaxf(row_max, largest(i));
+      for (int i = 0; i < NV; ++i) row_max = larger(row_max, largest(i));
       row_max = block_reduce<true>(row_max, part[1]);
       if (tid == 0) scale[blockIdx.x] = row_max / kE4m3Max;
     }
@@ -118,13 +126,13 @@ __global__ __launch_bounds__(1024) void residual_norm_kernel(const void* __restr
       if constexpr (kOut == NormOut::Groups) {
         // a group is `lanes` neighbouring lanes of one wave
         m = largest(i);
-        for (int o = 1; o < lanes; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+        for (int o = 1; o < lanes; o <<= 1) m = larger(m, __shfl_xor(m, o));
       }
       if (c >= n4) continue;
       const float sc = m / kE4m3Max;
       if (kOut == NormOut::Groups && c % lanes == 0) scale[(row + c) / lanes] = sc;
       auto code = [&](float v) {
-        v = sc > 0.f ? v / sc : 0.f;
+        v = sc == 0.f ? 0.f : v / sc;
         return v != v ? v : fminf(fmaxf(v, -kE4m3Max), kE4m3Max);
       };
       int packed = __builtin_amdgcn_cvt_pk_fp8_f32(code(s[i].x), code(s[i].y), 0, false);

@@ -119,6 +119,53 @@ def test_residual_norm_zero_rows_and_in_place(gpu):
     assert ops.residual_norm(hd[:0], y.to(DEV)[:0], w.to(DEV))["norm"].shape == (0, 64)
 
 
+@pytest.mark.parametrize("H", [64, 4352, 16640])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("group", [None, 32, 256, -1])
+def test_residual_norm_not_finite(gpu, group, dtype, H):
+    """NaN and infinities in the stream, the addend and the weight: not finite exactly where the formulas are."""
+    if group is not None and H % group:
+        group = 64
+    say("norm not finite", group, dtype, H)
+    gen = torch.Generator().manual_seed(H)
+    nan = float("nan")
+    h, y, w = torch.randn(9, H, generator=gen).to(dtype), torch.randn(9, H, generator=gen), torch.randn(H, generator=gen)
+    h[1, H - 1], h[2, 0], h[3, 33], y[4, H // 2], y[5, 1], h[6, :] = nan, INF, -INF, nan, INF, nan
+    h[7, 5], y[7, 5] = INF, -INF  # their sum is NaN
+    for weight in (w, torch.where(torch.arange(H) == 40, torch.tensor(INF), w), torch.where(torch.arange(H) == 40, torch.tensor(nan), w)):
+        weight = weight.to(dtype)
+        got = ops.residual_norm(h.to(DEV), y.to(DEV), weight.to(DEV), group=group)
+        with np.errstate(invalid="ignore", over="ignore"):
+            s, n = A.residual_norm(h.double().numpy(), y.double().numpy(), weight.double().numpy(), 1e-6)
+            assert np.array_equal(np.isfinite(got["hidden"].cpu().double().numpy()), np.isfinite(s))
+            # an infinity's row has an infinite mean: zeros beside it, NaN in its place
+            if group is None:
+                out = got["norm"].cpu().double().numpy()
+                assert np.array_equal(np.isnan(out), np.isnan(n)) and np.array_equal(np.isinf(out), np.isinf(n))
+                assert (out[n == 0] == 0).all()
+                continue
+            parts = n.reshape(9, -1, H if group < 0 else group)
+            scale = np.abs(parts).max(axis=2) / 448
+            code = np.where(scale[..., None] == 0, 0.0, parts / scale[..., None])
+        out, got_scale = got["codes"].cpu().double().numpy().reshape(parts.shape), got["scale"].cpu().double().numpy()
+        assert np.array_equal(np.isnan(got_scale), np.isnan(scale)) and np.array_equal(np.isinf(got_scale), np.isinf(scale))
+        assert np.array_equal(np.isnan(out), np.isnan(code))
+        sound = np.isfinite(scale)
+        assert (out[sound & (scale == 0)] == 0).all() and (got_scale[sound & (scale == 0)] == 0).all()
+        assert (np.abs(out[sound & (scale > 0)]).max(axis=1) == 448).all()
+        assert (out[np.isinf(scale)][np.isfinite(parts[np.isinf(scale)])] == 0).all()
+
+
+@pytest.mark.parametrize("group", [None, 32, -1])
+def test_residual_norm_zero_over_zero(gpu, group):
+    h = torch.zeros(2, 96, device=DEV)
+    h[1] = 1.0
+    got = ops.residual_norm(h, None, torch.ones(96, device=DEV), eps=0.0, group=group)
+    for name in ("norm",) if group is None else ("codes", "scale"):
+        out = got[name].float()
+        assert out[0].isnan().all() and out[1].isfinite().all()
+
+
 # ---------------------------------------------------------------------------
 # sampling
 # ---------------------------------------------------------------------------
