@@ -314,7 +314,8 @@ int32_t acceptmoe_moe_forward(const void* hidden, int32_t dtype, const void* w_g
  * projection in 16 significant bits (as two bf16 numbers); an activation past
  * bf16's largest number, or not finite, makes its token's outputs NaN.  Deterministic.
  *   H and I positive multiples of 32 up to 65536, 1 <= E <= ACCEPTMOE_MAX_EXPERTS,
- *   1 <= k <= ACCEPTMOE_MAX_TOPK, T * H < 2^31 - 8; T == 0 is a no-op.  workspace as for
+ *   1 <= k <= ACCEPTMOE_MAX_TOPK, T * H < 2^31 - 8, T * k <= 2^30 and
+ *   (T * k / 64 + E + 16) * ceil(max(I, H / 2) / 128) < 2^24; T == 0 is a no-op.  workspace as for
  *   acceptmoe_moe_forward, of acceptmoe_moe_forward_q4_workspace_size bytes.
  */
 size_t acceptmoe_q4_gate_up_bytes(int32_t E, int32_t I, int32_t H);

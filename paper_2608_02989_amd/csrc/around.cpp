@@ -245,8 +245,9 @@ int32_t acceptmoe_moe_forward_q4(const void* hidden, const void* w_gate_up, cons
   if (static_cast<long long>(T) * k > (1ll << 30) || static_cast<long long>(T) * H >= (1ll << 31) - 8)
     return fail(ACCEPTMOE_ERR_UNSUPPORTED, "forward_q4: T too large: hidden is addressed in 32 bits (T=%d k=%d H=%d)", T,
                 k, H);
-  if (static_cast<long long>((H / 4 + 255) / 256) * T >= (1ll << 31))
-    return fail(ACCEPTMOE_ERR_UNSUPPORTED, "forward_q4: T * ceil(H / 1024) must stay below 2^31 (T=%d H=%d)", T, H);
+  if (!amoe::forward_q4_grids_fit(T, H, I, E, k))
+    return fail(ACCEPTMOE_ERR_UNSUPPORTED, "forward_q4: T too large: a product takes fewer than 2^24 workgroups (T=%d k=%d I=%d H=%d)",
+                T, k, I, H);
   if (!hidden || !w_gate_up || !w_down || !topk_idx || !topk_gate || !out)
     return fail(ACCEPTMOE_ERR_INVALID_ARG, "forward_q4: null pointer");
   if (!aligned(hidden, 16) || !aligned(w_gate_up, 16) || !aligned(w_down, 16) || !aligned(out, 16))

@@ -95,6 +95,9 @@ size_t forward_workspace_bytes(int T, int H, int I, int E, int k, int is_bf16);
 void forward_carve(void* ws, ForwardParams& p);
 hipError_t launch_forward(ForwardParams p, hipStream_t stream);
 
+// A launch takes fewer than 2^32 threads in all.
+constexpr int max_workgroups(int threads) { return static_cast<int>(0xffffffffu / static_cast<unsigned>(threads)); }
+
 // ---- residual norm (norm.hip) ----
 constexpr int kMaxNormWidth = 65536;
 
@@ -153,6 +156,7 @@ hipError_t launch_pack_down_q4(const uint8_t* down, const uint8_t* down_scale, i
 hipError_t launch_quantize_q4(const void* w, int is_bf16, size_t groups, uint8_t* codes, uint8_t* scales,
                               hipStream_t stream);
 size_t forward_q4_workspace_bytes(int T, int H, int I, int E, int k);
+bool forward_q4_grids_fit(int T, int H, int I, int E, int k);
 void forward_q4_carve(void* ws, ForwardParams& p);
 hipError_t launch_forward_q4(ForwardParams p, hipStream_t stream);
 

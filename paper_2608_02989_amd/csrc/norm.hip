@@ -147,13 +147,24 @@ hipError_t launch_norm(const NormParams& p, int threads, hipStream_t stream) {
   const int n4 = p.H / 4;
   const float inv_h = 1.f / static_cast<float>(p.H);
   auto go = [&](auto kern, int lanes) {
-    kern<<<p.T, threads, 0, stream>>>(p.hidden, reinterpret_cast<const float4*>(p.y), p.weight, n4, inv_h, p.eps, lanes,
-                                      p.hidden_out, p.norm_out, p.scale);
+    const size_t eb = kBf16 ? 2 : 4, norm_eb = p.group == 0 ? eb : 1;
+    const int scales = p.group > 0 ? p.H / p.group : 1, most = max_workgroups(threads);
+    hipError_t err = hipSuccess;
+    for (int t0 = 0; t0 < p.T && err == hipSuccess; t0 += most) {
+      const size_t at = static_cast<size_t>(t0) * p.H;
+      kern<<<p.T - t0 < most ? p.T - t0 : most, threads, 0, stream>>>(
+          static_cast<const char*>(p.hidden) + at * eb, kAdd ? reinterpret_cast<const float4*>(p.y + at) : nullptr, p.weight,
+          n4, inv_h, p.eps, lanes, kAdd ? static_cast<char*>(p.hidden_out) + at * eb : nullptr,
+          static_cast<char*>(p.norm_out) + at * norm_eb,
+          p.group != 0 ? p.scale + static_cast<size_t>(t0) * scales : nullptr);
+      err = hipGetLastError();
+      if (p.T - t0 <= most) break;
+    }
+    return err;
   };
-  if (p.group == 0) go(&residual_norm_kernel<kBf16, kAdd, NV, NormOut::Plain>, 0);
-  else if (p.group > 0) go(&residual_norm_kernel<kBf16, kAdd, NV, NormOut::Groups>, p.group / 4);
-  else go(&residual_norm_kernel<kBf16, kAdd, NV, NormOut::Row>, 0);
-  return hipGetLastError();
+  if (p.group == 0) return go(&residual_norm_kernel<kBf16, kAdd, NV, NormOut::Plain>, 0);
+  if (p.group > 0) return go(&residual_norm_kernel<kBf16, kAdd, NV, NormOut::Groups>, p.group / 4);
+  return go(&residual_norm_kernel<kBf16, kAdd, NV, NormOut::Row>, 0);
 }
 
 template <bool kBf16, bool kAdd>

@@ -214,8 +214,8 @@ __global__ __launch_bounds__(kThreads) void q4_dispatch_kernel(ForwardParams p) 
 
 // out[t] = sum of the token's slot rows, in slot order
 template <int KMAX>
-__global__ __launch_bounds__(256) void q4_combine_kernel(ForwardParams p, int hblocks) {
-  const int t = blockIdx.x / hblocks;
+__global__ __launch_bounds__(256) void q4_combine_kernel(ForwardParams p, int hblocks, int t0) {
+  const int t = t0 + blockIdx.x / hblocks;
   const int c = (blockIdx.x % hblocks) * 256 + threadIdx.x, H4 = p.H / 4;
   if (c >= H4) return;
   int ev[KMAX];
@@ -500,6 +500,7 @@ __device__ __forceinline__ Q4Share q4_share(int b, int runs) {
   const int slot = b / 8;
   return {(slot / 2 / runs * 8 + b % 8) * 2 + (slot & 1), slot / 2 % runs};
 }
+constexpr int q4_runs(int quads) { return (quads + kQ4Waves - 1) / kQ4Waves; }
 long long q4_grid(int max_items, int runs) { return 16ll * ((max_items + 15) / 16) * runs; }
 
 template <bool kDown, int kRows>
@@ -507,7 +508,7 @@ __global__ __launch_bounds__(kQ4Waves* kWave) __attribute__((amdgpu_waves_per_eu
     ForwardParams p, int quads) {
   __shared__ uint4 lds[kQ4LdsPieces<kDown, kRows>];
   __shared__ Q4Rows qr;
-  const Q4Share sh = q4_share(blockIdx.x, (quads + kQ4Waves - 1) / kQ4Waves);
+  const Q4Share sh = q4_share(blockIdx.x, q4_runs(quads));
   if (sh.item >= *p.n_items) return;
   const int4 d = p.items[sh.item];
   const int e = __builtin_amdgcn_readfirstlane(d.x);
@@ -529,8 +530,7 @@ __global__ __launch_bounds__(kQ4Waves* kWave) __attribute__((amdgpu_waves_per_eu
 template <bool kDown, int kRows>
 hipError_t launch_q4_pass(const ForwardParams& p, hipStream_t stream) {
   const int quads = kDown ? q4_down_quads(p.H) : q4_gate_up_quads(p.I);
-  const long long grid = q4_grid(q4_max_items(p.T * p.k, p.E, p.item_rows), (quads + kQ4Waves - 1) / kQ4Waves);
-  if (grid > 0x7fffffffll) return hipErrorInvalidValue;  // far beyond one device's memory
+  const long long grid = q4_grid(q4_max_items(p.T * p.k, p.E, p.item_rows), q4_runs(quads));
   q4_kernel<kDown, kRows><<<static_cast<unsigned>(grid), kQ4Waves * kWave, 0, stream>>>(p, quads);
   return hipGetLastError();
 }
@@ -749,9 +749,13 @@ hipError_t launch_q4_dispatch(const ForwardParams& p, hipStream_t stream) {
 
 template <int KMAX>
 hipError_t launch_q4_combine(const ForwardParams& p, hipStream_t stream) {
-  const int hblocks = (p.H / 4 + 255) / 256;
-  q4_combine_kernel<KMAX><<<static_cast<unsigned>(hblocks) * static_cast<unsigned>(p.T), 256, 0, stream>>>(p, hblocks);
-  return hipGetLastError();
+  const int hblocks = (p.H / 4 + 255) / 256, most = max_workgroups(256) / hblocks;  // tokens of a launch
+  hipError_t err = hipSuccess;
+  for (int t0 = 0; t0 < p.T && err == hipSuccess; t0 += most) {
+    q4_combine_kernel<KMAX><<<hblocks * (p.T - t0 < most ? p.T - t0 : most), 256, 0, stream>>>(p, hblocks, t0);
+    err = hipGetLastError();
+  }
+  return err;
 }
 
 }  // namespace
@@ -820,6 +824,12 @@ static size_t q4_carve(char* c, int T, int H, int I, int E, int k, ForwardParams
 }
 
 size_t forward_q4_workspace_bytes(int T, int H, int I, int E, int k) { return q4_carve(nullptr, T, H, I, E, k, nullptr); }
+
+// The products' launches take the block (far beyond one device's memory they do not).
+bool forward_q4_grids_fit(int T, int H, int I, int E, int k) {
+  const int items = q4_max_items(T * k, E, q4_item_limit(T, k)), most = max_workgroups(kQ4Waves * kWave);
+  return q4_grid(items, q4_runs(q4_gate_up_quads(I))) <= most && q4_grid(items, q4_runs(q4_down_quads(H))) <= most;
+}
 
 void forward_q4_carve(void* ws, ForwardParams& p) { q4_carve(static_cast<char*>(ws), p.T, p.H, p.I, p.E, p.k, &p); }
 

@@ -108,6 +108,18 @@ def test_forward_q4_rejects(change, code, word):
     refused(fwd(**change), code, word)
 
 
+@pytest.mark.parametrize("change", [{"T": 1 << 25, "k": 32, "I": 128}, {"T": 1 << 25, "k": 8, "I": 1024, "H": 32},
+                                    {"T": 32767, "k": 32, "H": 65536, "I": 65536, "experts": 512, "nbytes": 100}])
+def test_forward_q4_more_workgroups_than_a_launch_takes(change):
+    """Refused before the first launch, also where T * ceil(H / 1024) is small."""
+    T, k, I, H, E = (change.get(n, d) for n, d in (("T", 4), ("k", 2), ("I", 32), ("H", 32), ("experts", 8)))
+    fits = (T * k // 64 + E + 16) * -(-max(I, H // 2) // 128) < 1 << 24
+    if fits:  # a large call that stays within the limits gets as far as its workspace
+        refused(fwd(**change), L.ERR_WORKSPACE, "needs")
+    else:
+        refused(fwd(**{"H": H, **change}), L.ERR_UNSUPPORTED, "workgroups")
+
+
 def test_q4_sizes():
     lib = L.lib()
     # a quad of 16-row tiles takes 4,352 bytes per 128 columns

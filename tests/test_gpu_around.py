@@ -102,6 +102,22 @@ def test_residual_norm_beyond_32_bits(gpu):
         del got
 
 
+@pytest.mark.parametrize("group", [None, -1])
+def test_residual_norm_more_rows_than_a_launch_takes(gpu, group):
+    """2^32 threads and more in all: rows of both launches as in a call of their own."""
+    T, H = 2 ** 26 + 70, 4
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    h = torch.randn(T, H, generator=gen, device=DEV).bfloat16()
+    w = torch.rand(H, generator=gen, device=DEV).bfloat16()
+    for add in (False, True):
+        y = torch.randn(T, H, generator=gen, device=DEV) if add else None
+        got = ops.residual_norm(h, y, w, group=group)
+        for part in (slice(0, 40), slice(2 ** 26 - 21, 2 ** 26 + 30), slice(T - 9, T)):
+            want = ops.residual_norm(h[part].clone(), None if y is None else y[part].clone(), w, group=group)
+            for name in want:
+                assert torch.equal(got[name][part].view(torch.uint8), want[name].view(torch.uint8)), (add, name, part)
+
+
 def test_residual_norm_zero_rows_and_in_place(gpu):
     h = torch.zeros(3, 64, dtype=torch.bfloat16)
     h[1] = 2.0

@@ -119,6 +119,25 @@ def test_forward_long_lists(gpu, T, H, I, E, k):
     run_check(T, H, I, E, k)
 
 
+def test_forward_more_tokens_than_a_launch_takes(gpu):
+    """2^24 tokens and more, each row a copy of one of the first 1000, some routed nowhere."""
+    T, few, H, I, E = 2 ** 24 + 1234, 1000, 32, 32, 3
+    stacks, x, idx, g = case(6, few, H, I, E, 1)
+    wgu, wd = packed(stacks)
+    ref, bound = forward_bound(x.double().numpy(), *[A.dequantize_q4(*s) for s in stacks], idx, g)
+    row = torch.arange(T, device=DEV) % few
+    out = torch.full((T, H), float("nan"), device=DEV)
+    ops.moe_forward_q4(x.to(DEV)[row], wgu, wd, dev(idx)[row], dev(g)[row], out=out)
+    worst = torch.zeros(few, H, dtype=torch.float64, device=DEV)
+    refd = dev(ref)
+    for a in range(0, T - T % few, 1000 * few):
+        part = out[a:min(a + 1000 * few, T - T % few)].view(-1, few, H).double()
+        worst = torch.maximum(worst, (part - refd).abs().amax(0))
+    tail = out[T - T % few:].double()
+    worst[:len(tail)] = torch.maximum(worst[:len(tail)], (tail - refd[:len(tail)]).abs())
+    assert (worst.cpu().numpy() <= bound).all()
+
+
 def test_forward_on_its_own_stream_and_in_a_graph(gpu):
     """Calls on a side stream with tensors of their own, and two captured graphs that share a
     workspace, replayed in turn with eager work between."""
