@@ -271,7 +271,8 @@ size_t acceptmoe_moe_forward_workspace_size(int32_t T, int32_t H, int32_t I, int
  *                 aligned, not shared by calls that may run concurrently
  *   Limits: H % 32 == 0 and I % 32 == 0 (bf16), H % 16 == 0 and I % 16 == 0
  *   (fp32); 1 <= E <= ACCEPTMOE_MAX_EXPERTS; 1 <= k <= ACCEPTMOE_MAX_TOPK;
- *   T == 0 is a no-op.
+ *   T * k <= 2^30, T * ceil(H / 1024) < 2^31 and fewer than 2^24 workgroups of
+ *   192 rows (fp32: 32) by 128 columns of I or 256 of H; T == 0 is a no-op.
  * bf16: MFMA bf16 products with fp32 accumulation; the SwiGLU activation is
  * rounded to bf16 before the down projection.  fp32: fp32 MFMA throughout.
  * The result is deterministic.  For T <= 256 with T*k <= 2048 the expert

@@ -253,6 +253,9 @@ int32_t acceptmoe_moe_forward(const void* hidden, int32_t dtype, const void* w_g
     return fail(ACCEPTMOE_ERR_UNSUPPORTED, "forward: T*k too large");
   if (static_cast<long long>((H / 4 + 255) / 256) * T >= (1ll << 31))
     return fail(ACCEPTMOE_ERR_UNSUPPORTED, "forward: T * ceil(H / 1024) must stay below 2^31 (T=%d H=%d)", T, H);
+  if (!amoe::grouped_grids_fit(T, H, I, E, k, dtype == ACCEPTMOE_BF16))
+    return fail(ACCEPTMOE_ERR_UNSUPPORTED, "forward: T too large: a product takes fewer than 2^24 workgroups (T=%d k=%d I=%d H=%d)",
+                T, k, I, H);
   if (!hidden || !w_gate_up || !w_down || !topk_idx || !topk_gate || !out)
     return fail(ACCEPTMOE_ERR_INVALID_ARG, "forward: null pointer");
   if (!aligned(hidden, 16) || !aligned(w_gate_up, 16) || !aligned(w_down, 16) || !aligned(out, 16))

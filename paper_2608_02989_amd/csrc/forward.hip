@@ -862,12 +862,11 @@ __global__ __launch_bounds__(kColLanes / NB * kWave) void down_col_kernel(Forwar
 // combine: out[t, h] = sum over the dispatched slots of token t, in slot order.
 // The routing row and all k expert rows are loaded before any is used (rows
 // of skipped slots are read but discarded).  Workgroup b covers token
-// b / hblocks, float4 columns 256 (b % hblocks) ..; a one-dimensional grid, so
-// any T fits.
+// t0 + b / hblocks, float4 columns 256 (b % hblocks) ..
 // ---------------------------------------------------------------------------
 template <int KMAX>
-__global__ __launch_bounds__(256) void combine_kernel(ForwardParams p, int hblocks) {
-  const int t = blockIdx.x / hblocks;
+__global__ __launch_bounds__(256) void combine_kernel(ForwardParams p, int hblocks, int t0) {
+  const int t = t0 + blockIdx.x / hblocks;
   const int h4 = (blockIdx.x % hblocks) * blockDim.x + threadIdx.x;  // float4 column
   const int H = p.H, k = p.k;
   if (h4 * 4 >= H) return;
@@ -1145,15 +1144,18 @@ hipError_t launch_forward(ForwardParams p, hipStream_t stream) {
   if (err != hipSuccess) return err;
   err = launch_grouped(p, max_grouped_items(p.T, p.E, p.k, p.is_bf16), stream);
   if (err != hipSuccess) return err;
-  const int hblocks = (p.H / 4 + 255) / 256;
-  const dim3 cgrid(static_cast<unsigned>(hblocks) * static_cast<unsigned>(p.T));
-  if (p.k <= 8)
-    combine_kernel<8><<<cgrid, 256, 0, stream>>>(p, hblocks);
-  else if (p.k <= 16)
-    combine_kernel<16><<<cgrid, 256, 0, stream>>>(p, hblocks);
-  else
-    combine_kernel<kMaxTopK><<<cgrid, 256, 0, stream>>>(p, hblocks);
-  return hipGetLastError();
+  const int hblocks = (p.H / 4 + 255) / 256, most = max_workgroups(256) / hblocks;  // tokens of a launch
+  for (int t0 = 0; t0 < p.T && err == hipSuccess; t0 += most) {
+    const int cgrid = hblocks * (p.T - t0 < most ? p.T - t0 : most);
+    if (p.k <= 8)
+      combine_kernel<8><<<cgrid, 256, 0, stream>>>(p, hblocks, t0);
+    else if (p.k <= 16)
+      combine_kernel<16><<<cgrid, 256, 0, stream>>>(p, hblocks, t0);
+    else
+      combine_kernel<kMaxTopK><<<cgrid, 256, 0, stream>>>(p, hblocks, t0);
+    err = hipGetLastError();
+  }
+  return err;
 }
 
 }  // namespace amoe

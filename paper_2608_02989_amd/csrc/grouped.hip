@@ -401,19 +401,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void g
 template <class P, Grouped F>
 hipError_t launch_grouped_pass(const ForwardParams& p, int max_items, int nblocks, hipStream_t stream) {
   const long long grid = grouped_workgroups(p.T * p.k, max_items, nblocks, P::kElemBytes);
-  // far beyond what the slot rows of one device's memory allow
-  if (grid > 0x7fffffffll) return hipErrorInvalidValue;
   grouped_kernel<P, F><<<static_cast<unsigned>(grid), 256, 0, stream>>>(p, nblocks, grouped_split_items(nblocks));
   return hipGetLastError();
 }
 
+constexpr int grouped_up_blocks(int I) { return (I / 16 + 7) / 8; }
+constexpr int grouped_down_blocks(int H) { return (H / 16 + 15) / 16; }
+
 template <class P>
 hipError_t launch_grouped_path(const ForwardParams& p, int max_items, hipStream_t stream) {
-  const hipError_t err = launch_grouped_pass<P, Grouped::GateUp>(p, max_items, (p.I / 16 + 7) / 8, stream);
-  return err != hipSuccess ? err : launch_grouped_pass<P, Grouped::Down>(p, max_items, (p.H / 16 + 15) / 16, stream);
+  const hipError_t err = launch_grouped_pass<P, Grouped::GateUp>(p, max_items, grouped_up_blocks(p.I), stream);
+  return err != hipSuccess ? err : launch_grouped_pass<P, Grouped::Down>(p, max_items, grouped_down_blocks(p.H), stream);
 }
 
 }  // namespace
+
+bool grouped_grids_fit(int T, int H, int I, int E, int k, int is_bf16) {
+  const int eb = is_bf16 ? 2 : 4, items = grouped_max_items(T * k, E, grouped_item_rows(eb));
+  const int most = max_workgroups(256);
+  return grouped_workgroups(T * k, items, grouped_up_blocks(I), eb) <= most &&
+         grouped_workgroups(T * k, items, grouped_down_blocks(H), eb) <= most;
+}
 
 hipError_t launch_grouped(const ForwardParams& p, int max_items, hipStream_t stream) {
   return p.is_bf16 ? launch_grouped_path<Bf16Path>(p, max_items, stream)

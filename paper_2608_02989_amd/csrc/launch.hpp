@@ -68,6 +68,10 @@ hipError_t launch_stream_read(const void* src, size_t bytes, uint32_t* sink, int
 hipError_t launch_pack_gate_up(const void* gate, const void* up, int is_bf16, int E, int I, int H, void* dst,
                                hipStream_t stream);
 
+// A launch takes fewer than 2^32 threads in all; of more the runtime starts the rest modulo
+// 2^32 without an error.
+constexpr int max_workgroups(int threads) { return static_cast<int>(0xffffffffu / static_cast<unsigned>(threads)); }
+
 struct ForwardParams {
   const void* hidden;
   const void* w_gate_up;  // packed gate/up tile pairs
@@ -90,13 +94,11 @@ struct ForwardParams {
 
 // grouped GEMMs of larger blocks (grouped.hip), both passes
 hipError_t launch_grouped(const ForwardParams& p, int max_items, hipStream_t stream);
+bool grouped_grids_fit(int T, int H, int I, int E, int k, int is_bf16);
 
 size_t forward_workspace_bytes(int T, int H, int I, int E, int k, int is_bf16);
 void forward_carve(void* ws, ForwardParams& p);
 hipError_t launch_forward(ForwardParams p, hipStream_t stream);
-
-// A launch takes fewer than 2^32 threads in all.
-constexpr int max_workgroups(int threads) { return static_cast<int>(0xffffffffu / static_cast<unsigned>(threads)); }
 
 // ---- residual norm (norm.hip) ----
 constexpr int kMaxNormWidth = 65536;

@@ -256,6 +256,12 @@ def test_forward_rejects():
     assert rc == L.ERR_UNSUPPORTED and "2^31" in msg, msg
 
 
+def test_forward_more_workgroups_than_a_launch_takes():
+    rc, msg = status_and_msg(fwd(T=1 << 25, H=256, I=4096, k=8))
+    assert rc == L.ERR_UNSUPPORTED and "workgroups" in msg, msg
+    assert fwd(T=1 << 25, H=256, I=256, k=1) == L.ERR_WORKSPACE
+
+
 def test_stream_read_rejects():
     f = L.lib().acceptmoe_stream_read
     assert f(FAKE, 1024, FAKE, 0, None) == L.ERR_INVALID_ARG           # grid < 1

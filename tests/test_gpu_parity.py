@@ -917,3 +917,28 @@ def test_graph_replay_matches_eager(gpu):
         got = snap()
         for a, b in zip(got, ref):
             assert torch.equal(a, b), f"replay {rep} differs"
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_forward_more_tokens_than_a_launch_takes(gpu, dtype):
+    """2^24 tokens and more, each row a copy of one of the first 1000, some routed nowhere."""
+    say("forward, many tokens", dtype)
+    T, few, H, I, E = 2 ** 24 + 1234, 1000, 32, 32, 3
+    gen = torch.Generator().manual_seed(7)
+    x = torch.randn(few, H, generator=gen).to(dtype)
+    wg, wu, wd = ((torch.randn(s, generator=gen) * 0.2).to(dtype) for s in ((E, I, H), (E, I, H), (E, H, I)))
+    idx = torch.randint(-1, E, (few, 1), generator=gen, dtype=torch.int32)
+    gate = torch.rand(few, 1, generator=gen)
+    row = torch.arange(T, device=DEV) % few
+    out = torch.full((T, H), float("nan"), device=DEV)
+    ops.moe_forward(x.to(DEV)[row], ops.pack_gate_up_weights(wg.to(DEV), wu.to(DEV)), ops.pack_expert_weights(wd.to(DEV)),
+                    idx.to(DEV)[row], gate.to(DEV)[row], out=out)
+    ref = torch.from_numpy(O.moe_forward_grouped(x.double().numpy(), *(w.float().numpy() for w in (wg, wu, wd)),
+                                                 idx.numpy(), gate.numpy())).to(DEV)
+    # a row's rounding relative to its largest output, as at the other shapes; I = 32 terms
+    tol = {torch.bfloat16: 1e-2, torch.float32: 1e-5}[dtype] * ref.abs().amax(1, keepdim=True)
+    whole = T - T % few
+    for a in range(0, whole, 1000 * few):
+        part = out[a:min(a + 1000 * few, whole)].view(-1, few, H).double()
+        assert ((part - ref).abs() <= tol).all(), a
+    assert ((out[whole:].double() - ref[:T - whole]).abs() <= tol[:T - whole]).all()
