@@ -994,7 +994,11 @@ __global__ __launch_bounds__(kPlaceThreads) void sample_place_kernel(SampleParam
     cut = first([&](double v) { return v >= want; }, kGridBins - 1);
   }
   if (rules.by_m()) {
-    const double t = grid_top - floor(grid.at(top) + kPerNat * log(rules.min_p));
+    // Where the border meets a bin's lower edge within rounding the next bin is looked at: its first
+    // tokens may weigh min_p in 64 bits (a temperature of 1e20 with min_p = 1: all weigh 1).
+    const double below = kPerNat * log(rules.min_p);
+    const double slack = (fabs(grid.at(top)) - below + 1.0) * 0x1p-50;
+    const double t = grid_top - floor(grid.at(top) + below - slack);
     if (t < (cut < 0 ? kGridBins : cut)) cut = static_cast<int>(t);
   }
   if (cut >= 0) {

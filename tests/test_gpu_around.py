@@ -369,6 +369,37 @@ def test_sample_settings_at_the_ends_of_their_types(gpu):
             assert (chosen > -INF).all() and ((prob > 0) & (prob <= 1)).all()
 
 
+@pytest.mark.parametrize("V", [70, 6000])
+@pytest.mark.parametrize("with_k", [True, False])
+def test_sample_defined_ends_of_settings(gpu, V, with_k):
+    """Settings at the ends of their types wherever the header says what they mean: token and probability of the oracle."""
+    tiny, nan = float(np.finfo(np.float32).smallest_subnormal), float("nan")
+    rows = [(t, p, m, k, u) for t in (1.0, tiny, 3e38, INF, nan, -INF) for p in (1.0, 0.57, 0.0, -INF, INF, tiny)
+            for m in (0.0, 0.5, INF, -INF) for k in ((0, 3, -2 ** 31, 2 ** 31 - 1) if with_k else (0,))
+            for u in (0.0, 0.7, INF, -1.0)]
+    t, p, m, k, u = (np.array(c, np.int32 if i == 3 else np.float32) for i, c in enumerate(zip(*rows)))
+    R = len(rows)
+    z = logits(np.random.default_rng(4), R, V)
+    z[::3, 5:60] = -INF
+    z[1::7, [9, 33]] = INF
+    z[2::5, 11] = nan
+    got = ops.sample(dev(z), dev(u), temperature=dev(t), top_p=dev(p), min_p=dev(m), **({"top_k": dev(k)} if with_k else {}))
+    token, prob = got["token"].cpu().numpy(), got["prob"].cpu().numpy()
+    unsure = 0
+    for r in range(R):
+        say("row", r, rows[r]) if r % 500 == 0 else None
+        # beside infinite logits every finite temperature gives the same weights, and so does the limit
+        tau = 1.0 if np.isposinf(t[r]) and np.isposinf(z[r]).any() else t[r]
+        want, prob_want, margin = A.sample_row(z[r], min(max(u[r], 0.0), 1 - 2.0 ** -24), temperature=tau, top_k=k[r],
+                                               top_p=p[r], min_p=m[r])
+        if margin <= 1:
+            unsure += 1
+            continue
+        assert token[r] == want, (rows[r], token[r], want, margin)
+        assert abs(prob[r] - prob_want) <= prob_want * (2.0 ** -24 + 1e-7), (rows[r], prob[r], prob_want)
+    assert unsure <= R // 50, unsure
+
+
 def test_sample_borders_of_u_and_top_p(gpu):
     z = np.log(np.tile(np.float32([4, 2, 1, 1]), (4, 1)))
     z = np.concatenate([z, np.full((4, 300), -INF, np.float32)], axis=1)
