@@ -294,7 +294,10 @@ int32_t acceptmoe_moe_forward(const void* hidden, int32_t dtype, const void* w_g
  * A weight is an e2m1 code (sign, 2 exponent bits, 1 mantissa bit: 0, 0.5, 1,
  * 1.5, 2, 3, 4, 6 for codes 0 .. 7, their negatives for 8 .. 15) times a power
  * of two shared by 32 neighbouring columns of its row, held as a byte s:
- *   W = code * 2^(s - 127),  2 <= s <= 252 (others: unspecified).
+ *   W = code * 2^(s - 127),  0 <= s <= 254; infinite past fp32's largest number (s = 253
+ *   and 254 with larger codes); s = 255 makes its 32 weights NaN.  Outputs that such a
+ *   weight enters are not finite, also through an activation of 0; in blocks of up to 32
+ *   routing entries it enters those of all tokens.
  * A stack [E, N, K] is two arrays: codes [E, N, K / 2] uint8, two a byte, the
  * lower nibble the column before, and scales [E, N, K / 32] uint8.
  *

@@ -269,7 +269,9 @@ __device__ __forceinline__ uint4 load_piece(const void* base, uint32_t bytes, ui
   return make_uint4(v.x, v.y, v.z, v.w);
 }
 
-// eight codes (low nibble first) times the scale, in bf16: exact for scale bytes 2 .. 252
+// Eight codes (low nibble first) times the scale, in bf16: exact (infinite past the largest
+// number).  The instruction takes the scale's exponent bits alone: byte 0, a scale of 0.0 as a
+// float, stands for 2^-127, byte 255 for NaN.
 __device__ __forceinline__ bf16x8 expand_q4(uint32_t codes, float scale) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);
@@ -549,7 +551,8 @@ hipError_t launch_q4_passes(const ForwardParams& p, hipStream_t stream) {
 //             gate * silu(g) * u (zeros where the token is not routed there) in two planes
 //   down      two workgroups per 16 columns over all experts: the chunks of all experts'
 //             K are dealt to their waves, and the sum over the experts happens in the MFMA's
-//             accumulators and then over the waves, in wave order; each adds its half onto the
+//             accumulators (zeros where a token is not routed: a weight that is not finite enters
+//             every token's sum) and then over the waves, in wave order; each adds its half onto the
 //             zeros that gate/up left in out (two additions onto zero commute: deterministic)
 // ---------------------------------------------------------------------------
 struct FewEntries {

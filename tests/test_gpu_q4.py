@@ -197,6 +197,73 @@ def test_forward_scales_across_the_range(gpu):
     assert (np.abs(got - ref) <= bound + I * 2.0 ** -126).all()
 
 
+@pytest.mark.parametrize("experts", [9, 16])
+@pytest.mark.parametrize("shift,first,last", [(20, 0, 200), (-20, 40, 255)])
+def test_forward_every_scale_byte(gpu, experts, shift, first, last):
+    """Row n of W_d has scale byte n, expert c code c in its first column alone: each output is one product, of
+    normal size for the bytes looked at.  9 experts, one token each, take the way without a dispatch."""
+    say("scale bytes", experts, shift)
+    H = 256
+    I = 32
+    rng = np.random.default_rng(5)
+    one = np.zeros((experts, I, H // 2), np.uint8)
+    one[:, 0, 0] = 2  # gate and up: 1.0 in the first row's first column
+    plain = np.full((experts, I, H // 32), 127, np.uint8)
+    down = np.zeros((experts, H, I // 2), np.uint8)
+    down[:, :, 0] = np.arange(experts)[:, None]
+    stacks = [(one, plain), (one, plain + np.uint8(shift % 256)),
+              (down, np.broadcast_to(np.arange(256, dtype=np.uint8)[None, :, None], (experts, H, 1)).copy())]
+    x = np.zeros((experts, H), np.float32)
+    x[:, 0] = 60.0 + rng.integers(0, 4, experts)
+    idx, g = np.arange(experts, dtype=np.int32)[:, None], np.ones((experts, 1), np.float32)
+    x = torch.from_numpy(x).bfloat16()
+    got = ops.moe_forward_q4(x.to(DEV), *packed(stacks), dev(idx), dev(g)).cpu().numpy()
+    w = [A.dequantize_q4(*s) for s in stacks]
+    ref, bound = forward_bound(x.double().numpy(), *w, idx, g)
+    sound = np.abs(w[2]).max(axis=2) <= np.finfo(np.float32).max  # [expert, row]
+    sound[:, 255] = False
+    if experts == 9:  # one sum over all experts, zeros for the tokens that are routed elsewhere
+        sound[:] = sound.all(axis=0)
+    rows = np.arange(first, last + 1)
+    ok = sound[:, rows]
+    size = np.abs(ref[:, rows])
+    assert (np.isfinite(got[:, rows]) == ok).all()
+    assert (np.abs(got[:, rows] - ref[:, rows])[ok] <= bound[:, rows][ok]).all()
+    # nothing passes for being small: 2^-126 is the smallest normal number
+    code = np.arange(experts) % 8 != 0
+    assert (size[code] > 2.0 ** -112).all() and (bound[:, rows] <= 2.0 ** -13 * size).all()
+
+
+def test_forward_scale_bytes_of_gate_and_up(gpu):
+    """Experts whose gate or up stack has one scale byte at an end of the range, against hidden states that bring
+    the products back to normal size."""
+    H = I = 64
+    ends = [(0, 118), (1, 118), (2, 117), (20, 100), (250, -118), (252, -120)]
+    cases = [(side, s, e) for side in (0, 1) for s, e in ends]
+    E = len(cases)
+    rng = np.random.default_rng(9)
+    stacks = [stack(rng, E, I, H), stack(rng, E, I, H), stack(rng, E, H, I)]
+    x = np.zeros((E, H), np.float32)
+    for c, (side, s, e) in enumerate(cases):
+        stacks[side][1][c] = s
+        stacks[1 - side][1][c] = 125 - e  # the other product: about 1
+        x[c] = rng.standard_normal(H) * 2.0 ** e
+    idx, g = np.arange(E, dtype=np.int32)[:, None], np.ones((E, 1), np.float32)
+    x = torch.from_numpy(x).bfloat16()
+    with np.errstate(over="ignore"):  # exp(-z) of a large -z
+        ref, bound = forward_bound(x.double().numpy(), *[A.dequantize_q4(*s) for s in stacks], idx, g)
+    for order in (np.arange(E), np.arange(9), np.arange(3, E)):  # with and without a dispatch
+        got = ops.moe_forward_q4(x[order].to(DEV), *packed(stacks), dev(idx[order]), dev(g[order])).cpu().numpy()
+        err = np.abs(got - ref[order])
+        say("gate and up bytes: error over bound", (err / bound[order]).max(axis=1))
+        assert (err <= bound[order]).all()
+    largest = np.abs(ref).max(axis=1)
+    assert (largest > 2.0 ** -60).all() and (bound.max(axis=1) < 0.01 * largest).all()
+    stacks[0][1][2] = 255  # NaN weights: their expert's token alone
+    got = ops.moe_forward_q4(x.to(DEV), *packed(stacks), dev(idx), dev(g)).cpu().numpy()
+    assert np.isnan(got[2]).all() and np.isfinite(np.delete(got, 2, axis=0)).all()
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_quantize(gpu, dtype):
     rng = np.random.default_rng(4)
