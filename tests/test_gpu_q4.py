@@ -170,6 +170,32 @@ def test_forward_on_its_own_stream_and_in_a_graph(gpu):
             ops.moe_forward_q4(xs[0], wgu, wd, i, gd)
 
 
+def test_forward_large_items_at_layer_width(gpu):
+    """Items of 48 and of 64 rows, several to an expert, at the width of a layer: a sample of the tokens, and that
+    equal tokens have equal rows."""
+    H, I, E, k, few = 2048, 768, 8, 4, 24
+    stacks, x, idx, g = case(77, few, H, I, E, k)
+    wgu, wd = packed(stacks)
+    ref, bound = forward_bound(x.double().numpy(), *[A.dequantize_q4(*s) for s in stacks], idx, g)
+    for T in (700, 1999, 2500):
+        row = torch.randint(0, few, (T,), generator=torch.Generator().manual_seed(T)).to(DEV)
+        got = ops.moe_forward_q4(x.to(DEV)[row], wgu, wd, dev(idx)[row], dev(g)[row]).cpu().numpy()
+        err = np.abs(got - ref[row.cpu()])
+        say(f"q4 T={T} at layer width: {(err / np.where(bound > 0, bound, 1)[row.cpu()]).max():.3f} of the bound")
+        assert (err <= bound[row.cpu()]).all()
+
+
+def test_layer_from_codes_and_scales(gpu):
+    """VerifyLayerQ4 given (codes, scales) pairs is the layer that quantises the stacks itself."""
+    cfg, [(layer, rw, _)] = small(1)
+    pairs = [ops.quantize_q4(w.float()) for w in W.expert_weights_torch(cfg, 0, DEV)]
+    other = ops.VerifyLayerQ4(dev(rw), *pairs, cfg.k, max_tokens=2 * cfg.T, max_trees=cfg.B)
+    blk = W.make_block(cfg, block=0)
+    args = [torch.from_numpy(blk.hidden).bfloat16().to(DEV)] + [dev(a) for a in (blk.parent, blk.depth, blk.prob)]
+    a, b = (ly.step(*args, tree_offsets=blk.offsets) for ly in (layer, other))
+    assert torch.equal(a[2], b[2]) and torch.equal(a[1]["idx"], b[1]["idx"])
+
+
 @pytest.mark.parametrize("T,H,I,E,k", [(4, 192, 160, 64, 6), (9, 192, 160, 64, 1), (10, 192, 160, 64, 1),
                                        (2, 320, 96, 64, 16), (1, 2048, 768, 64, 32), (3, 96, 224, 40, 10),
                                        (640, 160, 96, 8, 4), (641, 160, 96, 8, 4), (2048, 96, 64, 40, 4),
