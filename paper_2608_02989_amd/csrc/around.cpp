@@ -25,6 +25,8 @@ bool overlap(const void* a, size_t an, const void* b, size_t bn) {
   return x < y + bn && y < x + an;
 }
 
+static_assert(ACCEPTMOE_MAX_VOCAB == amoe::kMaxVocab, "the kernels' largest vocabulary");
+
 constexpr int kQ4MaxSize = 65536;  // a quad's run over K stays addressable by 32 bits
 
 bool q4_size(int32_t n) { return n >= 32 && n % 32 == 0 && n <= kQ4MaxSize; }

@@ -28,6 +28,7 @@ namespace {
 
 constexpr uint32_t kKeyNegInf = 0x007fffffu;  // logit_key(-inf); NaN gets key 0
 constexpr double kWeightOne = 8796093022208.0;  // 2^43
+static_assert(kMaxVocab <= 1 << 20, "a row's sum of weights of 2^43 fits 64 bits");
 
 __device__ __forceinline__ uint32_t token_key(float z) { return z != z ? 0u : logit_key(z); }
 
@@ -120,7 +121,7 @@ __device__ __forceinline__ void block_range(uint32_t& high, uint32_t& low, uint3
 }
 
 // ---------------------------------------------------------------------------
-// Any row, by one workgroup over the row in memory: a radix search by digits of 11,
+// Any row but a greedy one, by one workgroup over the row in memory: a radix search by digits of 11,
 // 11 and 10 bits of the key, with the weights (or counts) of each digit summed
 // in LDS.  (For all rows: 148 / 647 / 1221 us where the spread form below takes 17 / 51 / 58.)
 // ---------------------------------------------------------------------------
@@ -232,11 +233,6 @@ __device__ void sample_row(const SampleParams& p, int r, const Rules& rules, Row
   top = block_max(top, sh.part32);
   if (top <= kKeyNegInf) {  // no token left
     if (tid == 0) p.token[r] = -1, p.prob[r] = 0.f;
-    return;
-  }
-  if (rules.mode == Mode::Greedy) {
-    const int i = find_index(row, top, 1, sh);
-    if (tid == 0) p.token[r] = i, p.prob[r] = 1.f;
     return;
   }
   const RowRule rule{top, key_logit(top), rules.tau};
@@ -1390,9 +1386,12 @@ hipError_t launch_sample_type(const SampleParams& p, hipStream_t stream) {
 
 // One size for both types: an fp32 row has more splits.  Grows with R: a row is spread
 // over at most 8 workgroups or takes the splits of 32 tokens per thread.
+static constexpr int most_splits(int V) { return (V + 6) / 4 / (kScanThreads * 8) + 1; }
+static_assert(most_splits(kMaxVocab) <= kMaxSplits, "a row's splits: one per lane of a wave");
+
 size_t sample_workspace_bytes(int R, int V) {
   const size_t rows = R < kRowsPerLaunch ? R : kRowsPerLaunch;
-  const size_t whole = (V + 6) / 4 / (kScanThreads * 8) + 1;
+  const size_t whole = most_splits(V);
   return rows * sample_part_bytes(static_cast<int>(whole > 8 ? whole : 8));
 }
 
