@@ -313,7 +313,7 @@ int32_t acceptmoe_moe_forward(const void* hidden, int32_t dtype, const void* w_g
  * Rows and columns past the stack are zeros.  acceptmoe_q4_gate_up_bytes and
  * acceptmoe_q4_down_bytes give the sizes (0 for unsupported ones).
  * acceptmoe_moe_forward_q4 -- acceptmoe_moe_forward over such weights: hidden
- * [T, H] bf16, the same routing, out [T, H] fp32.  The products of the gate and up
+ * [T, H] bf16, the same routing, out [T, H] fp32 (overlaps no other argument).  The products of the gate and up
  * projections are exact with fp32 accumulation; the activation goes to the down
  * projection in 16 significant bits (as two bf16 numbers); an activation past
  * bf16's largest number, or not finite, makes its token's outputs NaN.  Deterministic.
@@ -364,7 +364,7 @@ int32_t acceptmoe_residual_add(const void* hidden, int32_t dtype, const float* y
  *               hidden_out is neither needed nor written
  *   weight      [H] device, `dtype`
  *   hidden_out  [T, H] device, `dtype`; may equal hidden
- *   norm_out    must overlap no input; scale_out is unused when group == 0
+ *   norm_out, scale_out  overlap no other argument; scale_out is unused when group == 0
  *   H % 4 == 0, H <= 65536, eps finite and >= 0; group 0, -1, 32, 64, 128 or 256
  *   and a divisor of H.  All pointers 16-byte aligned (scale_out: 4).
  * The sum of squares is held in fp32, in a fixed order (deterministic).  Values that are
@@ -427,7 +427,7 @@ int32_t acceptmoe_sample(const void* logits, int32_t dtype, int64_t row_stride, 
  *   length        [B] int32 device, written: nodes on the path (0: empty tree)
  *   bonus         [B] int32 device, written: target at the path's last node, the
  *                 token behind the accepted ones (-1: empty tree)
- * T == 0 with B == 0 is a no-op.
+ * The outputs overlap no other argument.  T == 0 with B == 0 is a no-op.
  */
 int32_t acceptmoe_accept(const int32_t* token, const int32_t* parent, const int32_t* target,
                          const int32_t* tree_offsets, int32_t B, int32_t T, uint8_t* on_path, int32_t* path,

@@ -77,6 +77,11 @@ int32_t acceptmoe_residual_norm(const void* hidden, int32_t dtype, const float* 
             overlap(hidden_out, n * eb, y, n * 4) || overlap(hidden_out, n * eb, weight, H * eb) ||
             overlap(hidden_out, n * eb, norm_out, norm_bytes)))
     return fail(ACCEPTMOE_ERR_INVALID_ARG, "residual_norm: hidden_out overlaps another argument");
+  const size_t scale_bytes = group == 0 ? 0 : static_cast<size_t>(T) * (group > 0 ? H / group : 1) * 4;
+  if (group != 0 && (overlap(scale_out, scale_bytes, hidden, n * eb) || (y && overlap(scale_out, scale_bytes, y, n * 4)) ||
+                     overlap(scale_out, scale_bytes, weight, H * eb) || overlap(scale_out, scale_bytes, norm_out, norm_bytes) ||
+                     (y && overlap(scale_out, scale_bytes, hidden_out, n * eb))))
+    return fail(ACCEPTMOE_ERR_INVALID_ARG, "residual_norm: scale_out overlaps another argument");
   const amoe::NormParams p = {hidden, y, weight, hidden_out, norm_out, scale_out, T, H, dtype == ACCEPTMOE_BF16, group,
                               eps};
   hipError_t e = amoe::launch_residual_norm(p, static_cast<hipStream_t>(stream));

@@ -36,6 +36,14 @@ def test_residual_norm_rejects(change, code, word):
     refused(norm(**change), code, word)
 
 
+@pytest.mark.parametrize("scale", [A, B, C, D, V(A.value + 4 * 64 * 2 - 4), V(D.value - 4)],
+                         ids=["hidden", "y", "weight", "norm_out", "hidden's end", "norm_out's start"])
+@pytest.mark.parametrize("group", [32, -1])
+def test_residual_norm_rejects_overlapping_scales(scale, group):
+    refused(norm(group=group, scale=scale), L.ERR_INVALID_ARG, "scale_out overlaps")
+    refused(norm(group=group, scale=scale, hidden_out=V(E.value + 0x10000000)), L.ERR_INVALID_ARG, "scale_out overlaps")
+
+
 def test_no_ops():
     assert norm(T=0) == L.OK
     assert sample(R=0) == L.OK
