@@ -1125,7 +1125,7 @@ __device__ __forceinline__ PlaceInList place_in_list(const Listed& l, int t0, do
   const int tid = threadIdx.x, lane = lane_id();
   const double unit = sh.step[t0] / kWeightOne;
   // an empty sum reaches nothing
-  auto reached = [&](unsigned long long sum) { return sum != 0 && passes(before + static_cast<double>(sum) * unit); };
+  auto reached = [&](unsigned long long sum) { return (sum != 0) & passes(before + static_cast<double>(sum) * unit); };
   // every token lies in [lo, hi): a list's keys share their upper bits
   uint32_t least = ~0u, most = 0;
 #pragma unroll
