@@ -401,8 +401,8 @@ int32_t acceptmoe_residual_norm(const void* hidden, int32_t dtype, const float* 
  *                not shared by calls that may run concurrently
  *   1 <= V <= ACCEPTMOE_MAX_VOCAB, R <= ACCEPTMOE_MAX_SAMPLE_ROWS; R == 0 is a no-op.
  * Exponentials and sums are held in 64 bits, so u falls between the borders that
- * 64-bit sums give (without top_k, weights below e^-31 of the largest may be left out
- * of the sums); the result is deterministic.
+ * 64-bit sums give, but for weights below 2^-44 of the largest, which may be left out
+ * of the sums; the result is deterministic.
  */
 size_t acceptmoe_sample_workspace_size(int32_t R, int32_t V);
 int32_t acceptmoe_sample(const void* logits, int32_t dtype, int64_t row_stride, int32_t R, int32_t V,

@@ -9,8 +9,8 @@
 // steps one after the other otherwise).  Nodes come behind their parents, so
 // an accepted node's place is the count of accepted nodes before it.
 //
-// Bound by latency: one workgroup per tree, three words a node (one tree of 64 nodes 2.7 us,
-// 32 of 60 3.5 us).
+// Bound by latency: one workgroup per tree, three words a node (one tree of 64 nodes 2.4 us,
+// 32 of 60 3.6 us).
 #include "common.hpp"
 #include "launch.hpp"
 

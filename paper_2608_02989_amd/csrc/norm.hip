@@ -6,9 +6,9 @@
 //   scale = max|n| / 448,  code = e4m3(n / scale).
 //
 // Bound by memory with many rows: every value is read and written once, 10 H bytes a row
-// in bf16 with an addend (16384 rows of 4096: 671 MB in 129 us, 5.2 TB/s, the rate of a large
-// copy).  1920 rows of 2048 to codes take 10.9 us (3.2 TB/s: 60 waves for
-// the 32 places of a CU, latency), one row 2.6 us.  256 threads a row: no difference.
+// in bf16 with an addend (16384 rows of 4096: 671 MB in 130 us, 5.2 TB/s, the rate of a large
+// copy).  1920 rows of 2048 to codes take 11.0 us a call (3.2 TB/s: 60 waves for
+// the 32 places of a CU, latency), one row 2.5 us.  256 threads a row: no difference.
 #include "common.hpp"
 #include "launch.hpp"
 

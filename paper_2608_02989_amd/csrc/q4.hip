@@ -4,17 +4,20 @@
 //   out_t = sum_j g_{t,j} W_d (silu(W_g x_t) * W_u x_t)
 //
 // Bound: with few rows per expert the weights' bytes (64 tokens in 26 experts, H = 4096,
-// I = 1536: gate/up 174 MB in 39 us, 4.5 TB/s, down 87 MB in 27 us), with many the matrix cores
+// I = 1536: gate/up 174 MB in 41 us, 4.3 TB/s, down 87 MB in 27 us), with many the matrix cores
 // and the expansion of the codes in front of them (1920 tokens, top-8, H = 2048, I = 768: 97
-// and, with the second plane, 97 GFLOP in 108 to 128 us each, 760 to 890 TFLOP/s of the 1248 that a large
-// bf16 product reaches), for a few tokens latency (one token: 6.3 and 5.7 us).
+// and, with the second plane, 97 GFLOP in 107 to 128 us each, 760 to 900 TFLOP/s of the 1248 that a large
+// bf16 product reaches), for a few tokens latency (one token: 6.2 and 6.0 us).
 //
 // Both factors of the gate and up products are exact in bf16 (a code has 2
 // significant bits, its scale is a power of two), so they run on the bf16 MFMA
 // with the weights expanded in registers.  The activation goes to the down
 // product as two bf16 planes, hi = bf16(a) and lo = bf16(a - hi), 16 bits of it
 // in all, which costs a second MFMA but no weight traffic: with hi alone every output
-// would carry up to 2^-8 from that one rounding, more than from all else together.
+// would carry up to 2^-8 from that one rounding, more than from all else together.  A third
+// plane would bring the error against 64 bits from 2.3e-6 .. 2.8e-6 to fp32's 0.6e-6 .. 1.2e-6, for
+// half of the down product's MFMAs again where these bound it; the blocks that latency or the weights'
+// bytes bound take the same two, so that precision does not depend on a block's size.
 //
 // Weights (pack_q4_kernel): per expert and quad of 16-row tiles one run over K;
 // per 128 columns four fragments of 64 lanes x 16 B and 64 lanes x 4 B of scales.

@@ -11,14 +11,16 @@
 //
 // Sums: the weights' exponentials are taken in 64 bits and held as whole numbers
 // of 2^-43, so a sum of up to 2^20 of them fits 64 bits, has no rounding and does
-// not depend on the order of the additions.
+// not depend on the order of the additions.  Bins of weights (below) are added up as
+// 64-bit floats, in a fixed order.
 //
 // Bound: with many rows the first pass over the logits (512 rows of 100003 in bf16, 102 MB:
-// 35.5 us of the call's 58, 2.9 TB/s, vector instructions per logit); with few the
+// 35.2 us of the call's 58, 2.9 TB/s; vector instructions take half of the SIMDs' cycles, and the
+// waves wait for loads and for the search's barriers 47 % of their time); with few the
 // latency of three or four launches of short dependent steps (one row of 32000: 6.3 us
-// for the pass, 9.7 for cutting and ordering its top 64, 2.5 for the launch that has
-// nothing left to do; 64 fp32 rows of 131072 with top-p alone: 13.9, 10.5, then 13.5 for the
-// second pass and 13.7 for the order within two bins).
+// for the pass, 9.8 for cutting and ordering its top 64, 2.6 for the launch that has
+// nothing left to do; 64 fp32 rows of 131072 with top-p alone: 14.6, 10.6, then 13.8 for the
+// second pass and 13.5 for the order within two bins).
 #include "common.hpp"
 #include "launch.hpp"
 
