@@ -271,8 +271,9 @@ size_t acceptmoe_moe_forward_workspace_size(int32_t T, int32_t H, int32_t I, int
  *                 aligned, not shared by calls that may run concurrently
  *   Limits: H % 32 == 0 and I % 32 == 0 (bf16), H % 16 == 0 and I % 16 == 0
  *   (fp32); 1 <= E <= ACCEPTMOE_MAX_EXPERTS; 1 <= k <= ACCEPTMOE_MAX_TOPK;
- *   T * k <= 2^30, T * ceil(H / 1024) < 2^31 and fewer than 2^24 workgroups of
- *   192 rows (fp32: 32) by 128 columns of I or 256 of H; T == 0 is a no-op.
+ *   T * k <= 2^30, T * ceil(H / 1024) < 2^31, and a product's workgroups below 2^24:
+ *   (T * k / 76 + E + 304) * ceil(max(I, H / 2) / 128) < 2^24 is enough (fp32: 21
+ *   instead of 76); T == 0 is a no-op.
  * bf16: MFMA bf16 products with fp32 accumulation; the SwiGLU activation is
  * rounded to bf16 before the down projection.  fp32: fp32 MFMA throughout.
  * The result is deterministic.  For T <= 256 with T*k <= 2048 the expert
@@ -296,8 +297,8 @@ int32_t acceptmoe_moe_forward(const void* hidden, int32_t dtype, const void* w_g
  * of two shared by 32 neighbouring columns of its row, held as a byte s:
  *   W = code * 2^(s - 127),  0 <= s <= 254; infinite past fp32's largest number (s = 253
  *   and 254 with larger codes); s = 255 makes its 32 weights NaN.  Outputs that such a
- *   weight enters are not finite, also through an activation of 0; in blocks of up to 32
- *   routing entries it enters those of all tokens.
+ *   weight enters are not finite, also through an activation of 0; in the smallest blocks
+ *   (at most 16 tokens and 32 routing entries) it may enter those of all tokens.
  * A stack [E, N, K] is two arrays: codes [E, N, K / 2] uint8, two a byte, the
  * lower nibble the column before, and scales [E, N, K / 32] uint8.
  *
